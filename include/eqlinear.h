@@ -309,6 +309,82 @@ eql_status_t eqlinear_step_host(eqlinear_plan_t plan, const void* x_host, const 
                                 void* dw_staging, void* db_staging,
                                 void* scratch, size_t scratch_bytes, void* stream);
 
+/* ---- optimiser step: AdamW over many tensors at once ------------------------------------------
+ * What turns dw and db (and every other gradient of a network) into the next parameters, which
+ * eqlinear_plan_set_weight then takes.  One call updates all tensors; one more, in front of it, bounds the global norm
+ * of the gradients, takes a loss scale out of them and skips the step where a gradient is not finite, without the host
+ * ever waiting.  (The paper trains with a framework's optimiser and says nothing of one; these entry points exist for
+ * the library's users.)  With f the factor of a preceding eqlinear_adamw_clip (else 1) and t the number of this step:
+ *
+ *     g' = f * g      m = beta1 * m + (1 - beta1) * g'      v = beta2 * v + (1 - beta2) * g'^2
+ *     p  = p * (1 - lr * lr_scale * weight_decay) - lr * lr_scale * (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ *
+ * all in float.  A tensor with a float `master` keeps its value there, and `param` receives it rounded to its type.
+ *
+ * States take 32 bits (float) or 8.  In 8 bits every 256 consecutive elements of a tensor share one float scale for m and
+ * one for v: m is held as e4m3 codes of m * (448 / max|m|) with scale max|m| / 448, v as e5m2 codes of v * (57344 / max v)
+ * with scale max v / 57344, both rounded to nearest even; a v above zero never becomes code zero (the least code, 2^-16,
+ * stands for it), so that a later step does not divide by nothing.  A block whose largest magnitude is below 2^-100 is held
+ * as zeros.  The step itself uses the states before they are rounded.  Zeroed codes and scales are valid initial states. */
+typedef struct eqlinear_adamw_s* eqlinear_adamw_t;   /* opaque host object */
+
+typedef struct {
+    void* param;              /* device [numel], param_dtype: read (unless there is a master) and written */
+    void* master;             /* device [numel] float, read and written; or NULL */
+    const void* grad;         /* device [numel], grad_dtype */
+    void* exp_avg;            /* device [numel]: m, float or e4m3 codes */
+    void* exp_avg_sq;         /* device [numel]: v, float or e5m2 codes */
+    float* exp_avg_scale;     /* device [ceil(numel / 256)], states in 8 bits only (4-byte aligned; else NULL) */
+    float* exp_avg_sq_scale;
+    int64_t numel;            /* >= 0; the pointers of an empty tensor are not looked at */
+    float weight_decay;       /* >= 0; 0 for biases and norms, usually */
+    float lr_scale;           /* factor of the step's learning rate for this tensor; 1 usually */
+    int32_t param_dtype, grad_dtype;      /* eql_dtype_t */
+} eql_adamw_tensor_t;
+
+typedef struct {
+    int64_t step;             /* steps taken: the next one is number step + 1 */
+    int64_t skipped;          /* steps left out because a gradient was not finite */
+    float grad_norm;          /* norm that the last eqlinear_adamw_clip saw (not finite where that was the reason) */
+    int32_t skip;             /* 1: the next eqlinear_adamw_step will be left out */
+} eql_adamw_info_t;
+
+/* Bytes of device workspace for these tensors; state_bits is 8 or 32. */
+eql_status_t eqlinear_adamw_workspace_bytes(const eql_adamw_tensor_t* tensors, int count, int state_bits, size_t* bytes);
+
+/* Build an optimiser on the current device over `count` tensors (host array, copied).  Its table of tensors and its step
+ * counter (0) live in `workspace` (device, 256-byte aligned, the caller's, untouched until eqlinear_adamw_destroy).  No two
+ * of the buffers that a step writes may share bytes, nor may one share bytes with a gradient or the workspace
+ * (EQL_ERR_INVALID_ARG).  The table travels over `stream`, which is synchronised: not during stream capture
+ * (EQL_ERR_INVALID_ARG).  On error *opt is set to NULL. */
+eql_status_t eqlinear_adamw(eqlinear_adamw_t* opt, const eql_adamw_tensor_t* tensors, int count, int state_bits,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* The global gradient norm, for the next eqlinear_adamw_step: with n = sqrt(sum of all g^2) / *loss_scale, that step uses
+ * f = min(1, max_norm / (n + 1e-6)) / *loss_scale, and is left out (no parameter, state or step number changes) where n or the
+ * loss scale is not finite or the loss scale is not above zero.
+ *   max_norm    > 0; infinity bounds nothing
+ *   loss_scale  device float, read when the kernel runs, or NULL for 1
+ *   norm        device float that receives n, or NULL
+ * Squares and sums are doubles, added in a fixed order: the same gradients give the same bits. */
+eql_status_t eqlinear_adamw_clip(eqlinear_adamw_t opt, float max_norm, const float* loss_scale, float* norm, void* stream);
+
+/* One step over all tensors (one kernel); uses up what eqlinear_adamw_clip left.
+ *   lr         >= 0, used unless lr_device is given: a device float, read when the kernel runs (schedules in captured graphs)
+ *   beta1, beta2 in [0, 1);  eps > 0
+ * The step number lives on the device and advances by itself, so a captured step can be replayed. */
+eql_status_t eqlinear_adamw_step(eqlinear_adamw_t opt, double lr, double beta1, double beta2, double eps,
+                                 const float* lr_device, void* stream);
+
+/* Sets the number of steps taken (asynchronous on `stream`), e.g. after loading a checkpoint; forgets a pending clip. */
+eql_status_t eqlinear_adamw_set_step(eqlinear_adamw_t opt, int64_t step, void* stream);
+
+/* Reads the counters back (synchronises `stream`). */
+eql_status_t eqlinear_adamw_info(eqlinear_adamw_t opt, eql_adamw_info_t* info, void* stream);
+
+/* Frees the host object only (the workspace is the caller's).  NULL is accepted. */
+eql_status_t eqlinear_adamw_destroy(eqlinear_adamw_t opt);
+
 #ifdef __cplusplus
 }
 #endif

@@ -2,6 +2,8 @@
 
 from . import binding, parallel, workloads  # noqa: F401
 from .binding import (  # noqa: F401
+    eqlinear_adamw, eqlinear_adamw_clip, eqlinear_adamw_destroy, eqlinear_adamw_info, eqlinear_adamw_set_step, eqlinear_adamw_step,
+    eqlinear_adamw_tensor, eqlinear_adamw_workspace_bytes,
     EQL_FLAG_CORRELATION, EQL_FLAG_FORCE_SIMT, EQL_FLAG_FORCE_STREAMING, EQL_FLAG_CTA_PAIR, EQL_FLAG_NO_CTA_PAIR, EQL_FLAG_GELU, EQL_FLAG_DIHEDRAL, EQL_BF16, EQL_FP16, EQL_FP32, EqlError,
     eqlinear_bwd_data, eqlinear_bwd_data_host, eqlinear_bwd_weight, eqlinear_bwd_weight_host,
     eqlinear_bwd_weight_from_spectrum, eqlinear_bwd_weight_scratch_bytes, eqlinear_bwd_weight_static, eqlinear_count_macs, eqlinear_fwd, eqlinear_fwd_host, eqlinear_fwd_save_spectrum, eqlinear_spectrum_bytes, eqlinear_plan,

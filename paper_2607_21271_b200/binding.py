@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, byref, c_char_p, c_int, c_int32, c_int64, c_size_t, c_uint, c_uint32, c_void_p
+from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_uint, c_uint32, c_void_p
 
 _PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG_DIR, "libeqlinear.so")
@@ -46,6 +46,8 @@ EXPORTED_SYMBOLS = (
     "eqlinear_spectrum_bytes", "eqlinear_fwd_save_spectrum", "eqlinear_bwd_weight_from_spectrum",
     "eqlinear_plan_clear_device_status", "eqlinear_plan_selftest_expired_wait", "eqlinear_plan_launch_counts",
     "eqlinear_workspace_bytes_flags",
+    "eqlinear_adamw_workspace_bytes", "eqlinear_adamw", "eqlinear_adamw_clip", "eqlinear_adamw_step", "eqlinear_adamw_set_step",
+    "eqlinear_adamw_info", "eqlinear_adamw_destroy",
 )
 
 
@@ -59,6 +61,18 @@ class EqlInfo(ctypes.Structure):
         ("bytes_per_token_bwd_weight", c_int64),
         ("workspace_bytes", c_size_t),
     ]
+
+
+class EqlAdamwTensor(ctypes.Structure):
+    _fields_ = [
+        ("param", c_void_p), ("master", c_void_p), ("grad", c_void_p), ("exp_avg", c_void_p), ("exp_avg_sq", c_void_p),
+        ("exp_avg_scale", c_void_p), ("exp_avg_sq_scale", c_void_p),
+        ("numel", c_int64), ("weight_decay", c_float), ("lr_scale", c_float), ("param_dtype", c_int32), ("grad_dtype", c_int32),
+    ]
+
+
+class EqlAdamwInfo(ctypes.Structure):
+    _fields_ = [("step", c_int64), ("skipped", c_int64), ("grad_norm", c_float), ("skip", c_int32)]
 
 
 class EqlError(RuntimeError):
@@ -108,6 +122,13 @@ def load_library(path: str | None = None) -> ctypes.CDLL:
         "eqlinear_spectrum_bytes": [V, I64, POINTER(SZ)],
         "eqlinear_fwd_save_spectrum": [V, V, V, I64, V, SZ, V],
         "eqlinear_bwd_weight_from_spectrum": [V, V, SZ, V, V, V, I64, V, SZ, V],
+        "eqlinear_adamw_workspace_bytes": [POINTER(EqlAdamwTensor), I, I, POINTER(SZ)],
+        "eqlinear_adamw": [POINTER(V), POINTER(EqlAdamwTensor), I, I, V, SZ, V],
+        "eqlinear_adamw_clip": [V, c_float, V, V, V],
+        "eqlinear_adamw_step": [V, c_double, c_double, c_double, c_double, V, V],
+        "eqlinear_adamw_set_step": [V, I64, V],
+        "eqlinear_adamw_info": [V, POINTER(EqlAdamwInfo), V],
+        "eqlinear_adamw_destroy": [V],
     }
     for name, argtypes in sigs.items():
         fn = getattr(lib, name)
@@ -267,3 +288,51 @@ def eqlinear_bwd_weight_static(plan, x, dy, dw, db, N, stream=0) -> None:
     32 MiB device array is used instead (shared by all calls; do not overlap two of them)."""
     _check(load_library().eqlinear_bwd_weight_static(plan, _ptr(x), _ptr(dy), _ptr(dw), _ptr(db), N, stream or None),
            "eqlinear_bwd_weight_static")
+
+
+def eqlinear_adamw_tensor(param, grad, exp_avg, exp_avg_sq, numel, param_dtype, grad_dtype, master=None, exp_avg_scale=None,
+                          exp_avg_sq_scale=None, weight_decay=0.0, lr_scale=1.0) -> EqlAdamwTensor:
+    """One tensor of an optimiser.  Only addresses are kept: the caller keeps the tensors alive."""
+    return EqlAdamwTensor(_ptr(param), _ptr(master), _ptr(grad), _ptr(exp_avg), _ptr(exp_avg_sq), _ptr(exp_avg_scale),
+                          _ptr(exp_avg_sq_scale), numel, weight_decay, lr_scale, param_dtype, grad_dtype)
+
+
+def _adamw_table(tensors):
+    return (EqlAdamwTensor * len(tensors))(*tensors)
+
+
+def eqlinear_adamw_workspace_bytes(tensors, state_bits: int) -> int:
+    out = c_size_t(0)
+    _check(load_library().eqlinear_adamw_workspace_bytes(_adamw_table(tensors), len(tensors), state_bits, byref(out)),
+           "eqlinear_adamw_workspace_bytes")
+    return out.value
+
+
+def eqlinear_adamw(tensors, state_bits: int, workspace, workspace_bytes: int, stream=0) -> int:
+    """Returns the opaque optimiser handle (an integer address)."""
+    h = c_void_p(None)
+    _check(load_library().eqlinear_adamw(byref(h), _adamw_table(tensors), len(tensors), state_bits, _ptr(workspace), workspace_bytes,
+                                         stream or None), "eqlinear_adamw")
+    return h.value
+
+
+def eqlinear_adamw_clip(opt, max_norm, loss_scale=None, norm=None, stream=0) -> None:
+    _check(load_library().eqlinear_adamw_clip(opt, max_norm, _ptr(loss_scale), _ptr(norm), stream or None), "eqlinear_adamw_clip")
+
+
+def eqlinear_adamw_step(opt, lr, beta1=0.9, beta2=0.999, eps=1e-8, lr_device=None, stream=0) -> None:
+    _check(load_library().eqlinear_adamw_step(opt, lr, beta1, beta2, eps, _ptr(lr_device), stream or None), "eqlinear_adamw_step")
+
+
+def eqlinear_adamw_set_step(opt, step, stream=0) -> None:
+    _check(load_library().eqlinear_adamw_set_step(opt, step, stream or None), "eqlinear_adamw_set_step")
+
+
+def eqlinear_adamw_info(opt, stream=0) -> EqlAdamwInfo:
+    info = EqlAdamwInfo()
+    _check(load_library().eqlinear_adamw_info(opt, byref(info), stream or None), "eqlinear_adamw_info")
+    return info
+
+
+def eqlinear_adamw_destroy(opt) -> None:
+    _check(load_library().eqlinear_adamw_destroy(opt), "eqlinear_adamw_destroy")

@@ -1,0 +1,562 @@
+// AdamW over many tensors in one launch, with states in 32 or in 8 bits, and the global gradient norm that may precede it.
+//
+// Everything here moves memory: per element a step reads the gradient, the two states and the parameter (or its float master) and
+// writes all but the gradient, 30 bytes with float states (float gradient, 16-bit parameter with master) or 18 with 8-bit ones, for
+// about 20 operations.  The unit of work is a chunk of 2048 elements of one tensor: eight warps, each one block of 256 elements, eight
+// per lane, so that the block that shares a scale is a warp and its maximum five shuffles.  The table of tensors and the
+// tensor of every chunk lie in the workspace; a CTA takes a contiguous run of chunks, and so meets a new tensor only now and then.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdlib>
+#include <new>
+
+#include "eql_internal.h"
+#include "ptx_sm100.cuh"
+
+namespace eql {
+namespace {
+
+constexpr int kBlock = 256;                 // elements that share a scale: one warp's
+constexpr int kAdamThreads = 256;
+constexpr int kChunk = kBlock * (kAdamThreads / 32);
+constexpr int kNormCtasPerSm = 4, kStepCtasPerSm = 3;
+constexpr int kMaxNormCtas = 1024;
+constexpr float kE4m3Max = 448.0f, kE5m2Max = 57344.0f, kE5m2Least = 0x1p-16f, kTiny = 0x1p-100f;
+
+// One tensor, as the kernels see it.
+struct Tensor {
+    void* param;
+    float* master;
+    const void* grad;
+    void *m, *v;
+    float *m_scale, *v_scale;
+    int64_t numel;
+    int32_t first_chunk;
+    int32_t param_dtype, grad_dtype;
+    float weight_decay, lr_scale;
+};
+
+// The optimiser's own state, at the start of the workspace.
+struct Control {
+    int64_t step, skipped;
+    float factor, norm;
+    int32_t skip;
+    unsigned step_ticket, norm_ticket;
+};
+static_assert(sizeof(Control) <= kWsAlign, "the control block has one slot of the workspace");
+
+struct Layout {
+    size_t partials, tensors, chunks, total;
+    int64_t n_chunks;
+};
+
+// What a step has in every element's formula (host: rounded once from double).
+struct Rates {
+    float lr, beta1, one_minus_beta1, beta2, one_minus_beta2, eps;
+    double log_beta1, log_beta2;
+    const float* lr_device;
+};
+
+// Eight elements of a lane: two runs of four, 128 elements apart, so that a warp's access is one run of 128 elements.
+__device__ __forceinline__ int lane_element(int lane, int j) { return (j >> 2) * 128 + lane * 4 + (j & 3); }
+
+// Four elements as they lie in memory (16 bytes of float, 8 of a 16-bit type), fetched before any of them is looked at.
+__device__ __forceinline__ uint4 load_raw4(const void* base, int64_t at, int dtype) {
+    if (dtype == EQL_FP32) return __ldcs(reinterpret_cast<const uint4*>(static_cast<const float*>(base) + at));
+    const uint2 u = __ldcs(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(base) + at));
+    return make_uint4(u.x, u.y, 0u, 0u);
+}
+__device__ __forceinline__ float widen16(uint32_t bits, int dtype) {
+    return dtype == EQL_FP16 ? __half2float(__ushort_as_half((unsigned short)bits)) : __uint_as_float(bits << 16);
+}
+__device__ __forceinline__ void widen4(const uint4& u, int dtype, float* f) {
+    if (dtype == EQL_FP32) {
+        f[0] = __uint_as_float(u.x); f[1] = __uint_as_float(u.y); f[2] = __uint_as_float(u.z); f[3] = __uint_as_float(u.w);
+    } else {
+        f[0] = widen16(u.x & 0xffffu, dtype); f[1] = widen16(u.x >> 16, dtype);
+        f[2] = widen16(u.y & 0xffffu, dtype); f[3] = widen16(u.y >> 16, dtype);
+    }
+}
+__device__ __forceinline__ float load_one(const void* base, int64_t at, int dtype) {
+    if (dtype == EQL_FP32) return static_cast<const float*>(base)[at];
+    return widen16(static_cast<const uint16_t*>(base)[at], dtype);
+}
+__device__ __forceinline__ uint32_t narrow16(float v, int dtype) {
+    return dtype == EQL_FP16 ? __half_as_ushort(__float2half_rn(v)) : __bfloat16_as_ushort(__float2bfloat16_rn(v));
+}
+__device__ __forceinline__ void store4(void* base, int64_t at, int dtype, const float* f) {
+    if (dtype == EQL_FP32)
+        __stcs(reinterpret_cast<float4*>(static_cast<float*>(base) + at), make_float4(f[0], f[1], f[2], f[3]));
+    else
+        __stcs(reinterpret_cast<uint2*>(static_cast<uint16_t*>(base) + at),
+               make_uint2(narrow16(f[0], dtype) | narrow16(f[1], dtype) << 16, narrow16(f[2], dtype) | narrow16(f[3], dtype) << 16));
+}
+__device__ __forceinline__ void store_one(void* base, int64_t at, int dtype, float f) {
+    if (dtype == EQL_FP32) static_cast<float*>(base)[at] = f;
+    else static_cast<uint16_t*>(base)[at] = (uint16_t)narrow16(f, dtype);
+}
+
+template <__nv_fp8_interpretation_t KIND>
+__device__ __forceinline__ void decode4(uint32_t codes, float scale, float* f) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(codes >> (16 * h)), KIND);
+        const float2 w = __half22float2(__half2(r));
+        f[2 * h] = __fmul_rn(w.x, scale);
+        f[2 * h + 1] = __fmul_rn(w.y, scale);
+    }
+}
+template <__nv_fp8_interpretation_t KIND>
+__device__ __forceinline__ uint32_t encode4(const float* q) {
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(q[0], q[1]), __NV_SATFINITE, KIND);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(q[2], q[3]), __NV_SATFINITE, KIND);
+    return lo | hi << 16;
+}
+
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
+    return v;
+}
+
+// The step, states of BITS bits.  The moments are computed by separately rounded operations: in 8 bits, what lies next to the border
+// of two codes goes by their last bit, and a plain program has to come to the same codes.  The denominator may be a few float
+// roundings off (approximate square root and division, about 2^-22): it moves the parameter by lr times that.
+template <int BITS>
+__global__ void __launch_bounds__(kAdamThreads) adamw_kernel(char* ws, Layout lay, Rates r) {
+    ptx::grid_handover();
+    Control* control = reinterpret_cast<Control*>(ws);
+    const Tensor* tensors = reinterpret_cast<const Tensor*>(ws + lay.tensors);
+    const int32_t* chunk_tensor = reinterpret_cast<const int32_t*>(ws + lay.chunks);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int32_t skip = control->skip;
+    if (!skip) {
+        const float factor = control->factor;
+        const double t = (double)(control->step + 1);
+        const float lr = r.lr_device ? *r.lr_device : r.lr;
+        const float correction1 = -expm1f((float)(t * r.log_beta1)), correction2 = -expm1f((float)(t * r.log_beta2));
+        const float root2 = rsqrtf(correction2);
+        const int64_t begin = lay.n_chunks * blockIdx.x / gridDim.x, end = lay.n_chunks * (blockIdx.x + 1) / gridDim.x;
+        int32_t which = -1;
+        Tensor x{};
+        for (int64_t c = begin; c < end; ++c) {
+            const int32_t now = chunk_tensor[c];
+            if (now != which) { x = tensors[now]; which = now; }
+            const int64_t base = (c - x.first_chunk) * kChunk + warp * kBlock;
+            const int64_t left = x.numel - base;
+            if (left <= 0) continue;
+            const float rate = lr * x.lr_scale, keep = 1.0f - rate * x.weight_decay, size = rate / correction1;
+            const bool full = left >= kBlock;
+            float g[8], m[8], v[8], p[8];
+            const void* from = x.master ? (const void*)x.master : (const void*)x.param;
+            const int from_dtype = x.master ? (int)EQL_FP32 : x.param_dtype;
+            const int64_t block = base / kBlock;
+            if (full) {
+                uint4 rg[2], rp[2], rm[2], rv[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int64_t at = base + h * 128 + lane * 4;
+                    rg[h] = load_raw4(x.grad, at, x.grad_dtype);
+                    rp[h] = load_raw4(from, at, from_dtype);
+                    if (BITS == 32) {
+                        rm[h] = load_raw4(x.m, at, EQL_FP32);
+                        rv[h] = load_raw4(x.v, at, EQL_FP32);
+                    } else {
+                        rm[h].x = __ldcs(reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(x.m) + at));
+                        rv[h].x = __ldcs(reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(x.v) + at));
+                    }
+                }
+                const float ms = BITS == 8 ? x.m_scale[block] : 0.0f, vs = BITS == 8 ? x.v_scale[block] : 0.0f;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    widen4(rg[h], x.grad_dtype, g + 4 * h);
+                    widen4(rp[h], from_dtype, p + 4 * h);
+                    if (BITS == 32) {
+                        widen4(rm[h], EQL_FP32, m + 4 * h);
+                        widen4(rv[h], EQL_FP32, v + 4 * h);
+                    } else {
+                        decode4<__NV_E4M3>(rm[h].x, ms, m + 4 * h);
+                        decode4<__NV_E5M2>(rv[h].x, vs, v + 4 * h);
+                    }
+                }
+            } else {
+                const float ms = BITS == 8 ? x.m_scale[block] : 0.0f, vs = BITS == 8 ? x.v_scale[block] : 0.0f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    g[j] = m[j] = v[j] = p[j] = 0.0f;
+                    const int64_t at = base + lane_element(lane, j);
+                    if (at >= x.numel) continue;
+                    g[j] = load_one(x.grad, at, x.grad_dtype);
+                    p[j] = load_one(from, at, from_dtype);
+                    if (BITS == 32) {
+                        m[j] = static_cast<const float*>(x.m)[at];
+                        v[j] = static_cast<const float*>(x.v)[at];
+                    } else {
+                        float f[4];
+                        decode4<__NV_E4M3>(static_cast<const uint8_t*>(x.m)[at], ms, f);
+                        m[j] = f[0];
+                        decode4<__NV_E5M2>(static_cast<const uint8_t*>(x.v)[at], vs, f);
+                        v[j] = f[0];
+                    }
+                }
+            }
+            float most_m = 0.0f, most_v = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float gs = __fmul_rn(g[j], factor);
+                m[j] = __fadd_rn(__fmul_rn(m[j], r.beta1), __fmul_rn(gs, r.one_minus_beta1));
+                v[j] = __fadd_rn(__fmul_rn(v[j], r.beta2), __fmul_rn(__fmul_rn(gs, gs), r.one_minus_beta2));
+                most_m = fmaxf(most_m, fabsf(m[j]));
+                most_v = fmaxf(most_v, v[j]);
+                float root;
+                asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(v[j]));
+                p[j] = p[j] * keep - __fdividef(size * m[j], root * root2 + r.eps);
+            }
+            float qm[8], qv[8];
+            if (BITS == 8) {
+                most_m = warp_max(most_m);
+                most_v = warp_max(most_v);
+                const bool fine_m = most_m >= kTiny, fine_v = most_v >= kTiny;
+                const float im = fine_m ? __fdiv_rn(kE4m3Max, most_m) : 0.0f, iv = fine_v ? __fdiv_rn(kE5m2Max, most_v) : 0.0f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    qm[j] = __fmul_rn(m[j], im);
+                    qv[j] = __fmul_rn(v[j], iv);
+                    if (fine_v && v[j] > 0.0f) qv[j] = fmaxf(qv[j], kE5m2Least);
+                }
+                if (lane == 0) {
+                    x.m_scale[block] = fine_m ? __fdiv_rn(most_m, kE4m3Max) : 0.0f;
+                    x.v_scale[block] = fine_v ? __fdiv_rn(most_v, kE5m2Max) : 0.0f;
+                }
+            }
+            if (full) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int64_t at = base + h * 128 + lane * 4;
+                    if (x.master) store4(x.master, at, EQL_FP32, p + 4 * h);
+                    store4(x.param, at, x.param_dtype, p + 4 * h);
+                    if (BITS == 32) {
+                        store4(x.m, at, EQL_FP32, m + 4 * h);
+                        store4(x.v, at, EQL_FP32, v + 4 * h);
+                    } else {
+                        __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(x.m) + at), encode4<__NV_E4M3>(qm + 4 * h));
+                        __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(x.v) + at), encode4<__NV_E5M2>(qv + 4 * h));
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int64_t at = base + lane_element(lane, j);
+                    if (at >= x.numel) continue;
+                    if (x.master) x.master[at] = p[j];
+                    store_one(x.param, at, x.param_dtype, p[j]);
+                    if (BITS == 32) {
+                        static_cast<float*>(x.m)[at] = m[j];
+                        static_cast<float*>(x.v)[at] = v[j];
+                    } else {
+                        static_cast<uint8_t*>(x.m)[at] = __nv_cvt_float_to_fp8(qm[j], __NV_SATFINITE, __NV_E4M3);
+                        static_cast<uint8_t*>(x.v)[at] = __nv_cvt_float_to_fp8(qv[j], __NV_SATFINITE, __NV_E5M2);
+                    }
+                }
+            }
+        }
+    }
+    // The last CTA to come here, when every CTA has read the control block, turns it to the next step.
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __threadfence();
+        if (atomicAdd(&control->step_ticket, 1u) == gridDim.x - 1) {
+            if (skip) control->skipped += 1;
+            else control->step += 1;
+            control->factor = 1.0f;
+            control->skip = 0;
+            control->step_ticket = 0;
+        }
+    }
+}
+
+__device__ __forceinline__ double cta_sum(double v, double* shared) {
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = v;
+    __syncthreads();
+    double s = 0.0;
+    for (int w = 0; w < kAdamThreads / 32; ++w) s += shared[w];
+    return s;
+}
+
+// Sum of squares in double: a float's square is exact there and no sum overflows, so the total is finite exactly where every gradient
+// is, and its rounding to float does not depend on the order of the sum (but for one in 10^8).  The last CTA adds the CTAs' sums
+// in the order of their numbers.
+__global__ void __launch_bounds__(kAdamThreads) grad_norm_kernel(char* ws, Layout lay, float max_norm, const float* loss_scale, float* norm_out) {
+    ptx::grid_handover();
+    Control* control = reinterpret_cast<Control*>(ws);
+    const Tensor* tensors = reinterpret_cast<const Tensor*>(ws + lay.tensors);
+    const int32_t* chunk_tensor = reinterpret_cast<const int32_t*>(ws + lay.chunks);
+    double* partials = reinterpret_cast<double*>(ws + lay.partials);
+    __shared__ double shared[kAdamThreads / 32];
+    __shared__ bool last;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t begin = lay.n_chunks * blockIdx.x / gridDim.x, end = lay.n_chunks * (blockIdx.x + 1) / gridDim.x;
+    double sum = 0.0;
+    int32_t which = -1;
+    const void* grad = nullptr;
+    int64_t numel = 0, first = 0;
+    int dtype = 0;
+    for (int64_t c = begin; c < end; ++c) {
+        const int32_t now = chunk_tensor[c];
+        if (now != which) {
+            which = now;
+            grad = tensors[now].grad; numel = tensors[now].numel; first = tensors[now].first_chunk; dtype = tensors[now].grad_dtype;
+        }
+        const int64_t base = (c - first) * kChunk + warp * kBlock;
+        if (numel - base >= kBlock) {
+            uint4 u[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) u[h] = load_raw4(grad, base + h * 128 + lane * 4, dtype);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float f[4];
+                widen4(u[h], dtype, f);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum = fma((double)f[j], (double)f[j], sum);
+            }
+        } else {
+            for (int j = 0; j < 8; ++j) {
+                const int64_t at = base + lane_element(lane, j);
+                if (at < numel) {
+                    const double f = load_one(grad, at, dtype);
+                    sum = fma(f, f, sum);
+                }
+            }
+        }
+    }
+    sum = cta_sum(sum, shared);
+    if (threadIdx.x == 0) {
+        partials[blockIdx.x] = sum;
+        __threadfence();
+        last = atomicAdd(&control->norm_ticket, 1u) == gridDim.x - 1;
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    sum = 0.0;
+    for (int i = threadIdx.x; i < (int)gridDim.x; i += kAdamThreads) sum += __ldcg(partials + i);
+    sum = cta_sum(sum, shared);
+    if (threadIdx.x == 0) {
+        const float scale = loss_scale ? *loss_scale : 1.0f;
+        const float norm = (float)(sqrt(sum) / (double)scale);
+        const bool fine = isfinite(norm) && isfinite(scale) && scale > 0.0f;
+        control->norm = norm;
+        control->skip = fine ? 0 : 1;
+        control->factor = fine ? __fdiv_rn(fminf(1.0f, __fdiv_rn(max_norm, __fadd_rn(norm, 1e-6f))), scale) : 0.0f;
+        control->norm_ticket = 0;
+        if (norm_out) *norm_out = norm;
+    }
+}
+
+__global__ void set_step_kernel(char* ws, int64_t step) {
+    Control* control = reinterpret_cast<Control*>(ws);
+    control->step = step;
+    control->factor = 1.0f;
+    control->skip = 0;
+}
+
+inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+inline bool known_dtype(int d) { return d == EQL_FP32 || d == EQL_FP16 || d == EQL_BF16; }
+inline int64_t chunks_of(int64_t numel) { return (numel + kChunk - 1) / kChunk; }
+
+eql_status_t layout(const eql_adamw_tensor_t* tensors, int count, int state_bits, Layout* lay) {
+    if (!tensors || count < 1 || (state_bits != 8 && state_bits != 32)) return EQL_ERR_INVALID_ARG;
+    if (count > 1 << 20) return EQL_ERR_UNSUPPORTED;
+    int64_t chunks = 0;
+    for (int i = 0; i < count; ++i) {
+        if (tensors[i].numel < 0) return EQL_ERR_INVALID_ARG;
+        if (tensors[i].numel > (int64_t)1 << 40) return EQL_ERR_UNSUPPORTED;
+        chunks += chunks_of(tensors[i].numel);
+    }
+    if (chunks > ((int64_t)1 << 31) - 1) return EQL_ERR_UNSUPPORTED;
+    lay->n_chunks = chunks;
+    lay->partials = kWsAlign;
+    lay->tensors = lay->partials + kMaxNormCtas * sizeof(double);
+    lay->chunks = align_up(lay->tensors + (size_t)count * sizeof(Tensor), kWsAlign);
+    lay->total = align_up(lay->chunks + (size_t)chunks * sizeof(int32_t), kWsAlign);
+    return EQL_OK;
+}
+
+struct Range {
+    uintptr_t begin, end;
+    bool written;
+};
+
+eql_status_t check_tensor(const eql_adamw_tensor_t& t, int state_bits, Range* ranges, int* n) {
+    if (!known_dtype(t.param_dtype) || !known_dtype(t.grad_dtype)) return EQL_ERR_INVALID_ARG;
+    if (!(t.weight_decay >= 0.0f) || !std::isfinite(t.weight_decay) || !std::isfinite(t.lr_scale)) return EQL_ERR_INVALID_ARG;
+    if (t.numel == 0) return EQL_OK;
+    if (!t.param || !t.grad || !t.exp_avg || !t.exp_avg_sq) return EQL_ERR_INVALID_ARG;
+    if ((state_bits == 8) != (t.exp_avg_scale != nullptr) || (state_bits == 8) != (t.exp_avg_sq_scale != nullptr)) return EQL_ERR_INVALID_ARG;
+    if (!aligned(t.param, 16) || !aligned(t.master, 16) || !aligned(t.grad, 16) || !aligned(t.exp_avg, 16) || !aligned(t.exp_avg_sq, 16) ||
+        !aligned(t.exp_avg_scale, 4) || !aligned(t.exp_avg_sq_scale, 4))
+        return EQL_ERR_ALIGNMENT;
+    const int64_t blocks = (t.numel + kBlock - 1) / kBlock;
+    auto add = [&](const void* p, int64_t bytes, bool written) {
+        if (p) ranges[(*n)++] = Range{(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, written};
+    };
+    add(t.param, t.numel * (t.param_dtype == EQL_FP32 ? 4 : 2), true);
+    add(t.master, t.numel * 4, true);
+    add(t.grad, t.numel * (t.grad_dtype == EQL_FP32 ? 4 : 2), false);
+    add(t.exp_avg, t.numel * (state_bits / 8), true);
+    add(t.exp_avg_sq, t.numel * (state_bits / 8), true);
+    add(t.exp_avg_scale, blocks * 4, true);
+    add(t.exp_avg_sq_scale, blocks * 4, true);
+    return EQL_OK;
+}
+
+// Whether a written range shares bytes with any other.
+bool ranges_clash(Range* ranges, int n) {
+    std::sort(ranges, ranges + n, [](const Range& a, const Range& b) { return a.begin < b.begin; });
+    uintptr_t end = 0, end_written = 0;
+    for (int i = 0; i < n; ++i) {
+        if (ranges[i].begin < (ranges[i].written ? end : end_written)) return true;
+        end = std::max(end, ranges[i].end);
+        if (ranges[i].written) end_written = std::max(end_written, ranges[i].end);
+    }
+    return false;
+}
+
+}  // namespace
+}  // namespace eql
+
+// The host object behind eqlinear_adamw_t.
+struct eqlinear_adamw_s {
+    int device, num_sms, state_bits;
+    char* ws;
+    eql::Layout lay;
+};
+
+namespace {
+
+using namespace eql;
+
+eql_status_t check_optimiser(eqlinear_adamw_t opt) {
+    if (!opt) return EQL_ERR_INVALID_ARG;
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) return EQL_ERR_CUDA;
+    return dev == opt->device ? EQL_OK : EQL_ERR_INVALID_ARG;
+}
+
+}  // namespace
+
+extern "C" {
+
+eql_status_t eqlinear_adamw_workspace_bytes(const eql_adamw_tensor_t* tensors, int count, int state_bits, size_t* bytes) {
+    if (!bytes) return EQL_ERR_INVALID_ARG;
+    Layout lay{};
+    if (eql_status_t st = layout(tensors, count, state_bits, &lay); st != EQL_OK) return st;
+    *bytes = lay.total;
+    return EQL_OK;
+}
+
+eql_status_t eqlinear_adamw(eqlinear_adamw_t* opt, const eql_adamw_tensor_t* tensors, int count, int state_bits, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+    if (!opt) return EQL_ERR_INVALID_ARG;
+    *opt = nullptr;
+    Layout lay{};
+    if (eql_status_t st = layout(tensors, count, state_bits, &lay); st != EQL_OK) return st;
+    if (!workspace) return EQL_ERR_INVALID_ARG;
+    if (!aligned(workspace, kWsAlign)) return EQL_ERR_ALIGNMENT;
+    if (workspace_bytes < lay.total) return EQL_ERR_WORKSPACE;
+    Range* ranges = new (std::nothrow) Range[(size_t)count * 7 + 1];
+    if (!ranges) return EQL_ERR_INVALID_ARG;
+    int n = 0;
+    ranges[n++] = Range{(uintptr_t)workspace, (uintptr_t)workspace + lay.total, true};
+    eql_status_t st = EQL_OK;
+    for (int i = 0; i < count && st == EQL_OK; ++i) st = check_tensor(tensors[i], state_bits, ranges, &n);
+    if (st == EQL_OK && ranges_clash(ranges, n)) st = EQL_ERR_INVALID_ARG;
+    delete[] ranges;
+    if (st != EQL_OK) return st;
+
+    int dev = 0, major = 0, sms = kNumSMs;
+    if (cudaGetDevice(&dev) != cudaSuccess) return EQL_ERR_CUDA;
+    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) return EQL_ERR_CUDA;
+    if (major != 10) return EQL_ERR_ARCH;
+    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return EQL_ERR_CUDA;
+    const cudaStream_t s = (cudaStream_t)stream;
+    cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(s, &capturing) != cudaSuccess) return EQL_ERR_CUDA;
+    if (capturing != cudaStreamCaptureStatusNone) return EQL_ERR_INVALID_ARG;
+
+    char* image = static_cast<char*>(std::calloc(1, lay.total));
+    if (!image) return EQL_ERR_INVALID_ARG;
+    reinterpret_cast<Control*>(image)->factor = 1.0f;
+    Tensor* table = reinterpret_cast<Tensor*>(image + lay.tensors);
+    int32_t* chunk_tensor = reinterpret_cast<int32_t*>(image + lay.chunks);
+    int64_t chunk = 0;
+    for (int i = 0; i < count; ++i) {
+        const eql_adamw_tensor_t& t = tensors[i];
+        table[i] = Tensor{t.param, (float*)t.master, t.grad, t.exp_avg, t.exp_avg_sq, t.exp_avg_scale, t.exp_avg_sq_scale, t.numel, (int32_t)chunk,
+                          t.param_dtype, t.grad_dtype, t.weight_decay, t.lr_scale};
+        for (int64_t k = chunks_of(t.numel); k > 0; --k) chunk_tensor[chunk++] = i;
+    }
+    cudaError_t e = cudaMemcpyAsync(workspace, image, lay.total, cudaMemcpyHostToDevice, s);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    std::free(image);
+    if (e != cudaSuccess) return EQL_ERR_CUDA;
+    eqlinear_adamw_s* o = new (std::nothrow) eqlinear_adamw_s{dev, sms, state_bits, (char*)workspace, lay};
+    if (!o) return EQL_ERR_INVALID_ARG;
+    *opt = o;
+    return EQL_OK;
+}
+
+eql_status_t eqlinear_adamw_clip(eqlinear_adamw_t opt, float max_norm, const float* loss_scale, float* norm, void* stream) {
+    if (eql_status_t st = check_optimiser(opt); st != EQL_OK) return st;
+    if (!(max_norm > 0.0f)) return EQL_ERR_INVALID_ARG;
+    if (!aligned(loss_scale, 4) || !aligned(norm, 4)) return EQL_ERR_ALIGNMENT;
+    const int64_t most = std::min(opt->num_sms * kNormCtasPerSm, kMaxNormCtas);
+    const unsigned grid = (unsigned)std::max<int64_t>(1, std::min(opt->lay.n_chunks, most));
+    cudaError_t e = launch_overlapped(grad_norm_kernel, dim3(grid), dim3(kAdamThreads), 0, (cudaStream_t)stream, opt->ws, opt->lay, max_norm,
+                                      loss_scale, norm);
+    return e == cudaSuccess ? EQL_OK : EQL_ERR_CUDA;
+}
+
+eql_status_t eqlinear_adamw_step(eqlinear_adamw_t opt, double lr, double beta1, double beta2, double eps, const float* lr_device, void* stream) {
+    if (eql_status_t st = check_optimiser(opt); st != EQL_OK) return st;
+    if (!(lr >= 0.0) || !std::isfinite(lr) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0)) return EQL_ERR_INVALID_ARG;
+    if (!((float)eps > 0.0f) || !std::isfinite((float)eps)) return EQL_ERR_INVALID_ARG;
+    if (!aligned(lr_device, 4)) return EQL_ERR_ALIGNMENT;
+    const Rates r{(float)lr, (float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps, std::log(beta1), std::log(beta2), lr_device};
+    const int64_t most = (int64_t)opt->num_sms * kStepCtasPerSm;
+    const unsigned grid = (unsigned)std::max<int64_t>(1, std::min(opt->lay.n_chunks, most));
+    cudaError_t e = launch_overlapped(opt->state_bits == 8 ? adamw_kernel<8> : adamw_kernel<32>, dim3(grid), dim3(kAdamThreads), 0, (cudaStream_t)stream,
+                                      opt->ws, opt->lay, r);
+    return e == cudaSuccess ? EQL_OK : EQL_ERR_CUDA;
+}
+
+eql_status_t eqlinear_adamw_set_step(eqlinear_adamw_t opt, int64_t step, void* stream) {
+    if (eql_status_t st = check_optimiser(opt); st != EQL_OK) return st;
+    if (step < 0) return EQL_ERR_INVALID_ARG;
+    set_step_kernel<<<1, 1, 0, (cudaStream_t)stream>>>(opt->ws, step);
+    return cudaGetLastError() == cudaSuccess ? EQL_OK : EQL_ERR_CUDA;
+}
+
+eql_status_t eqlinear_adamw_info(eqlinear_adamw_t opt, eql_adamw_info_t* info, void* stream) {
+    if (eql_status_t st = check_optimiser(opt); st != EQL_OK) return st;
+    if (!info) return EQL_ERR_INVALID_ARG;
+    Control c{};
+    if (cudaMemcpyAsync(&c, opt->ws, sizeof(c), cudaMemcpyDeviceToHost, (cudaStream_t)stream) != cudaSuccess) return EQL_ERR_CUDA;
+    if (cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess) return EQL_ERR_CUDA;
+    *info = eql_adamw_info_t{c.step, c.skipped, c.norm, c.skip};
+    return EQL_OK;
+}
+
+eql_status_t eqlinear_adamw_destroy(eqlinear_adamw_t opt) {
+    delete opt;
+    return EQL_OK;
+}
+
+}  // extern "C"
