@@ -309,6 +309,51 @@ eql_status_t eqlinear_step_host(eqlinear_plan_t plan, const void* x_host, const 
                                 void* dw_staging, void* db_staging,
                                 void* scratch, size_t scratch_bytes, void* stream);
 
+/* ---- group norm with an activation, channels last ----------------------------------------------
+ * What stands between two layers of a network: a norm over features [B, S, C*T] (B instances of S positions; group index
+ * fastest) and a pointwise activation.  Both keep a layer's equivariance, because gamma and beta are per CHANNEL, shared by
+ * the T elements of its tuple, and statistics run over all of them.  (The paper's networks have such layers between its
+ * linear ones and leave them to a framework.)  With the C channels in `groups` runs of C / groups, and n_b positions of instance b:
+ *
+ *     mean, var over the n_b * (C / groups) * T elements of an instance and group;  rstd = 1 / sqrt(var + eps)
+ *     xh = (x - mean) * rstd     z = gamma[c] * xh + beta[c]     y = act(z)
+ *
+ * S = 1 is the norm of every token by itself (groups = 1: layer norm); T = 1 the ordinary group norm.  Statistics,
+ * sums and everything between input and output are float; y and dx are rounded once. */
+typedef enum { EQL_ACT_NONE = 0, EQL_ACT_GELU = 1 /* z * Phi(z), exact form */, EQL_ACT_SILU = 2 /* z / (1 + exp(-z)) */ } eql_act_t;
+
+typedef struct {
+    int32_t T;                /* elements of a channel's tuple: the layer's T, for a dihedral layer 2T; 1 to 64 */
+    int32_t C, groups;        /* channels; groups divides C.  C * T * elem is a multiple of 16 bytes */
+    int32_t dtype;            /* eql_dtype_t of x, y, dy, dx, gamma, beta */
+    int32_t act;              /* eql_act_t */
+    float eps;                /* > 0 */
+    int64_t batch, positions; /* B and S, >= 0 */
+} eql_groupnorm_t;
+
+/* Bytes of device scratch either direction needs at most (0 is possible). */
+eql_status_t eqlinear_groupnorm_scratch_bytes(const eql_groupnorm_t* norm, size_t* bytes);
+
+/* Forward.
+ *   x, y         device [B, S, C*T]
+ *   gamma, beta  device [C], or NULL for ones / zeros
+ *   lengths      device int32 [B], or NULL: n_b = lengths[b], taken as 0 below 0 and S above S (NULL: S).  Rows from n_b on are
+ *                padding: not read, and left as they are in y.  An instance without rows has mean 0 and var 0
+ *   stats        device float [B, groups, 2], receives mean and rstd for the backward pass; or NULL
+ *   scratch      device, 256-byte aligned, contents undefined afterwards; may be NULL where scratch_bytes may be 0 */
+eql_status_t eqlinear_groupnorm_fwd(const eql_groupnorm_t* norm, const void* x, const void* gamma, const void* beta, const int32_t* lengths,
+                                    void* y, float* stats, void* scratch, size_t scratch_bytes, void* stream);
+
+/* Gradients, from x and the stats that the forward pass saved (with dz = dy * act'(z), z computed again):
+ *     dbeta[c] = sum of dz,  dgamma[c] = sum of dz * xh,  over instances, positions and tuple
+ *     dx = rstd * (gamma * dz - (s1 + xh * s2) / (n_b * C / groups * T)),  s1, s2: sums of gamma * dz and gamma * dz * xh over the group
+ *   dx              device [B, S, C*T]; rows of padding are left as they are
+ *   dgamma, dbeta   device float [C], overwritten; either may be NULL
+ * Sums run in a fixed order: results are the same bits from run to run. */
+eql_status_t eqlinear_groupnorm_bwd(const eql_groupnorm_t* norm, const void* x, const void* dy, const void* gamma, const void* beta,
+                                    const int32_t* lengths, const float* stats, void* dx, void* dgamma, void* dbeta,
+                                    void* scratch, size_t scratch_bytes, void* stream);
+
 /* ---- optimiser step: AdamW over many tensors at once ------------------------------------------
  * What turns dw and db (and every other gradient of a network) into the next parameters, which
  * eqlinear_plan_set_weight then takes.  One call updates all tensors; one more, in front of it, bounds the global norm

@@ -2,6 +2,8 @@
 
 from . import binding, parallel, workloads  # noqa: F401
 from .binding import (  # noqa: F401
+    EQL_ACT_GELU, EQL_ACT_NONE, EQL_ACT_SILU,
+    eqlinear_groupnorm_bwd, eqlinear_groupnorm_desc, eqlinear_groupnorm_fwd, eqlinear_groupnorm_scratch_bytes,
     eqlinear_adamw, eqlinear_adamw_clip, eqlinear_adamw_destroy, eqlinear_adamw_info, eqlinear_adamw_set_step, eqlinear_adamw_step,
     eqlinear_adamw_tensor, eqlinear_adamw_workspace_bytes,
     EQL_FLAG_CORRELATION, EQL_FLAG_FORCE_SIMT, EQL_FLAG_FORCE_STREAMING, EQL_FLAG_CTA_PAIR, EQL_FLAG_NO_CTA_PAIR, EQL_FLAG_GELU, EQL_FLAG_DIHEDRAL, EQL_BF16, EQL_FP16, EQL_FP32, EqlError,

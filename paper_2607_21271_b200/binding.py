@@ -35,6 +35,10 @@ EQL_FLAG_NO_CTA_PAIR = 16
 EQL_FLAG_GELU = 32
 EQL_FLAG_DIHEDRAL = 64
 
+EQL_ACT_NONE = 0
+EQL_ACT_GELU = 1
+EQL_ACT_SILU = 2
+
 EQL_STATIC_SCRATCH_BYTES = 32 << 20
 
 # Every symbol include/eqlinear.h declares.
@@ -46,6 +50,7 @@ EXPORTED_SYMBOLS = (
     "eqlinear_spectrum_bytes", "eqlinear_fwd_save_spectrum", "eqlinear_bwd_weight_from_spectrum",
     "eqlinear_plan_clear_device_status", "eqlinear_plan_selftest_expired_wait", "eqlinear_plan_launch_counts",
     "eqlinear_workspace_bytes_flags",
+    "eqlinear_groupnorm_scratch_bytes", "eqlinear_groupnorm_fwd", "eqlinear_groupnorm_bwd",
     "eqlinear_adamw_workspace_bytes", "eqlinear_adamw", "eqlinear_adamw_clip", "eqlinear_adamw_step", "eqlinear_adamw_set_step",
     "eqlinear_adamw_info", "eqlinear_adamw_destroy",
 )
@@ -60,6 +65,13 @@ class EqlInfo(ctypes.Structure):
         ("bytes_per_token_fwd", c_int64), ("bytes_per_token_bwd_data", c_int64),
         ("bytes_per_token_bwd_weight", c_int64),
         ("workspace_bytes", c_size_t),
+    ]
+
+
+class EqlGroupnorm(ctypes.Structure):
+    _fields_ = [
+        ("T", c_int32), ("C", c_int32), ("groups", c_int32), ("dtype", c_int32), ("act", c_int32), ("eps", c_float),
+        ("batch", c_int64), ("positions", c_int64),
     ]
 
 
@@ -122,6 +134,9 @@ def load_library(path: str | None = None) -> ctypes.CDLL:
         "eqlinear_spectrum_bytes": [V, I64, POINTER(SZ)],
         "eqlinear_fwd_save_spectrum": [V, V, V, I64, V, SZ, V],
         "eqlinear_bwd_weight_from_spectrum": [V, V, SZ, V, V, V, I64, V, SZ, V],
+        "eqlinear_groupnorm_scratch_bytes": [POINTER(EqlGroupnorm), POINTER(SZ)],
+        "eqlinear_groupnorm_fwd": [POINTER(EqlGroupnorm), V, V, V, V, V, V, V, SZ, V],
+        "eqlinear_groupnorm_bwd": [POINTER(EqlGroupnorm), V, V, V, V, V, V, V, V, V, V, SZ, V],
         "eqlinear_adamw_workspace_bytes": [POINTER(EqlAdamwTensor), I, I, POINTER(SZ)],
         "eqlinear_adamw": [POINTER(V), POINTER(EqlAdamwTensor), I, I, V, SZ, V],
         "eqlinear_adamw_clip": [V, c_float, V, V, V],
@@ -288,6 +303,28 @@ def eqlinear_bwd_weight_static(plan, x, dy, dw, db, N, stream=0) -> None:
     32 MiB device array is used instead (shared by all calls; do not overlap two of them)."""
     _check(load_library().eqlinear_bwd_weight_static(plan, _ptr(x), _ptr(dy), _ptr(dw), _ptr(db), N, stream or None),
            "eqlinear_bwd_weight_static")
+
+
+def eqlinear_groupnorm_desc(T, C, groups, dtype, batch, positions, act=EQL_ACT_NONE, eps=1e-5) -> EqlGroupnorm:
+    """Shape of a norm over features [batch, positions, C*T]; checked by the calls that take it."""
+    return EqlGroupnorm(T, C, groups, dtype, act, eps, batch, positions)
+
+
+def eqlinear_groupnorm_scratch_bytes(norm) -> int:
+    out = c_size_t(0)
+    _check(load_library().eqlinear_groupnorm_scratch_bytes(byref(norm), byref(out)), "eqlinear_groupnorm_scratch_bytes")
+    return out.value
+
+
+def eqlinear_groupnorm_fwd(norm, x, gamma, beta, lengths, y, stats, scratch, scratch_bytes, stream=0) -> None:
+    _check(load_library().eqlinear_groupnorm_fwd(byref(norm), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(lengths), _ptr(y), _ptr(stats),
+                                                 _ptr(scratch), scratch_bytes, stream or None), "eqlinear_groupnorm_fwd")
+
+
+def eqlinear_groupnorm_bwd(norm, x, dy, gamma, beta, lengths, stats, dx, dgamma, dbeta, scratch, scratch_bytes, stream=0) -> None:
+    _check(load_library().eqlinear_groupnorm_bwd(byref(norm), _ptr(x), _ptr(dy), _ptr(gamma), _ptr(beta), _ptr(lengths), _ptr(stats),
+                                                 _ptr(dx), _ptr(dgamma), _ptr(dbeta), _ptr(scratch), scratch_bytes, stream or None),
+           "eqlinear_groupnorm_bwd")
 
 
 def eqlinear_adamw_tensor(param, grad, exp_avg, exp_avg_sq, numel, param_dtype, grad_dtype, master=None, exp_avg_scale=None,

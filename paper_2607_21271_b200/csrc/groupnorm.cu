@@ -1,0 +1,418 @@
+// Group norm with an activation, forward and backward: kernels that go through global memory between statistics and result, and the
+// C entry points.
+//
+// These kernels take every shape.  A CTA works on a piece of up to 256 vectors of a row, over a range of rows of one instance; a thread
+// stays with one vector column, so that what belongs to a column (statistics, gamma, sums) lies in its registers however
+// the borders of channels and groups fall.  Forward: moments of every column and row range, their merging to groups, and a pass that
+// applies them; backward: sums of dz and dz * xh of every column and row range, their merging to channels and groups, a pass that
+// applies them, and the sum over instances.  x (and dy) are read twice.
+#include <cmath>
+
+#include "groupnorm_common.cuh"
+
+namespace eql {
+namespace {
+
+constexpr int kThreads = 256;
+
+// Row ranges and pieces of an instance.
+struct Ranges {
+    int pieces, ranges;       // pieces of a row, ranges of rows
+    int64_t rows;             // rows of a range
+    float* columns;           // float2 [B][ranges][D], a column's partial of a range
+    float* groups;            // float2 [B][groups]: forward mean and rstd, backward the two means that dx takes off
+    float* channels;          // float2 [B][C], backward
+};
+
+struct Place {
+    int64_t b, row0;
+    int rows, range, vector, lane, lanes;
+    bool active;
+};
+// blockIdx.x = (b * ranges + range) * pieces + piece
+__device__ __forceinline__ Place place(const NormShape& s, const Ranges& g, const int32_t* lengths) {
+    Place p;
+    const int64_t unit = blockIdx.x / (unsigned)g.pieces;
+    const int first = (int)(blockIdx.x % (unsigned)g.pieces) * kThreads, count = min(kThreads, s.vectors - first);
+    p.b = unit / g.ranges;
+    p.range = (int)(unit % g.ranges);
+    p.lanes = kThreads / count;
+    p.lane = threadIdx.x / count;
+    p.vector = first + threadIdx.x % count;
+    p.active = p.lane < p.lanes;
+    p.row0 = p.range * g.rows;
+    const int64_t left = positions_of(lengths, p.b, s.S) - p.row0;
+    p.rows = (int)(left < 0 ? 0 : left < g.rows ? left : g.rows);
+    return p;
+}
+
+template <typename IO>
+__global__ void __launch_bounds__(kThreads) column_moments_kernel(NormShape s, Ranges g, const uint4* x, const int32_t* lengths) {
+    constexpr int V = NormIo<IO>::kVec;
+    ptx::grid_handover();
+    __shared__ float2 shared[kThreads * V];
+    const Place p = place(s, g, lengths);
+    RunningMoments<V> m;
+    if (p.active) {
+        const uint4* at = x + (p.b * s.S + p.row0 + p.lane) * s.vectors + p.vector;
+        for (int r = p.lane; r < p.rows; r += p.lanes, at += (int64_t)p.lanes * s.vectors) {
+            float f[V];
+            NormIo<IO>::widen(*at, f);
+            m.add(f);
+        }
+    }
+    const int count = min(kThreads, s.vectors - (int)(blockIdx.x % (unsigned)g.pieces) * kThreads);
+    auto rows_of = [&](int lane) { return (float)((p.rows - lane + p.lanes - 1) / p.lanes); };
+    if (p.active) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) shared[threadIdx.x * V + j] = make_float2(m.mean[j], m.m2[j]);
+    }
+    __syncthreads();
+    const int first = (int)(blockIdx.x % (unsigned)g.pieces) * kThreads * V;
+    float2* out = reinterpret_cast<float2*>(g.columns) + (p.b * g.ranges + p.range) * s.D + first;
+    for (int c = threadIdx.x; c < count * V; c += kThreads) {
+        Moments all{0.0f, 0.0f, 0.0f};
+        for (int l = 0; l < p.lanes && l < p.rows; ++l) {
+            const float2 v = shared[l * count * V + c];
+            all = merge(all, Moments{rows_of(l), v.x, v.y});
+        }
+        out[c] = make_float2(all.mean, all.m2);
+    }
+}
+
+// One CTA an instance and group.
+__global__ void __launch_bounds__(kThreads) group_moments_kernel(NormShape s, Ranges g, const int32_t* lengths, float* stats) {
+    ptx::grid_handover();
+    __shared__ Moments shared[kThreads / 32];
+    const int64_t b = blockIdx.x / (unsigned)s.groups;
+    const int group = (int)(blockIdx.x % (unsigned)s.groups);
+    const int64_t n = positions_of(lengths, b, s.S);
+    const float2* columns = reinterpret_cast<const float2*>(g.columns) + b * g.ranges * s.D + group * s.width;
+    Moments all{0.0f, 0.0f, 0.0f};
+    for (int64_t i = threadIdx.x; i < (int64_t)g.ranges * s.width; i += kThreads) {
+        const int64_t range = i / s.width, left = n - range * g.rows;
+        const float rows = (float)(left < 0 ? 0 : left < g.rows ? left : g.rows);
+        const float2 v = columns[range * s.D + i % s.width];
+        all = merge(all, Moments{rows, v.x, v.y});
+    }
+    all = warp_merge(all);
+    if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = all;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kThreads / 32; ++w) all = merge(all, shared[w]);
+        const float2 out = make_float2(all.mean, rstd_of(all, s.eps));
+        reinterpret_cast<float2*>(g.groups)[blockIdx.x] = out;
+        if (stats) reinterpret_cast<float2*>(stats)[blockIdx.x] = out;
+    }
+}
+
+// What a thread keeps of its column: the group's mean and rstd, gamma and beta.
+template <typename IO>
+struct Column {
+    static constexpr int V = NormIo<IO>::kVec;
+    float mean[V], rstd[V], gamma[V], beta[V];
+    __device__ __forceinline__ Column(const NormShape& s, const float2* stats, const IO* gammas, const IO* betas, int64_t b, int vector) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int e = vector * V + j, channel = e / s.T;
+            const float2 st = stats[b * s.groups + e / s.width];
+            mean[j] = st.x; rstd[j] = st.y;
+            gamma[j] = gammas ? NormIo<IO>::one(gammas, channel) : 1.0f;
+            beta[j] = betas ? NormIo<IO>::one(betas, channel) : 0.0f;
+        }
+    }
+};
+
+template <typename IO, int ACT>
+__global__ void __launch_bounds__(kThreads) apply_kernel(NormShape s, Ranges g, const uint4* x, const IO* gamma, const IO* beta,
+                                                         const int32_t* lengths, uint4* y) {
+    constexpr int V = NormIo<IO>::kVec;
+    ptx::grid_handover();
+    const Place p = place(s, g, lengths);
+    if (!p.active || p.lane >= p.rows) return;
+    Column<IO> c(s, reinterpret_cast<const float2*>(g.groups), gamma, beta, p.b, p.vector);
+#pragma unroll
+    for (int j = 0; j < V; ++j) c.gamma[j] *= c.rstd[j];
+    int64_t at = (p.b * s.S + p.row0 + p.lane) * s.vectors + p.vector;
+    for (int r = p.lane; r < p.rows; r += p.lanes, at += (int64_t)p.lanes * s.vectors) {
+        float f[V];
+        NormIo<IO>::widen(x[at], f);
+#pragma unroll
+        for (int j = 0; j < V; ++j) f[j] = activate<ACT>(fmaf(f[j] - c.mean[j], c.gamma[j], c.beta[j]));
+        y[at] = NormIo<IO>::narrow(f);
+    }
+}
+
+template <typename IO, int ACT>
+__global__ void __launch_bounds__(kThreads) column_sums_kernel(NormShape s, Ranges g, const uint4* x, const uint4* dy, const IO* gamma, const IO* beta,
+                                                               const int32_t* lengths, const float* stats) {
+    constexpr int V = NormIo<IO>::kVec;
+    ptx::grid_handover();
+    __shared__ float2 shared[kThreads * V];
+    const Place p = place(s, g, lengths);
+    float db[V] = {}, dg[V] = {};
+    if (p.active && p.lane < p.rows) {
+        const Column<IO> c(s, reinterpret_cast<const float2*>(stats), gamma, beta, p.b, p.vector);
+        int64_t at = (p.b * s.S + p.row0 + p.lane) * s.vectors + p.vector;
+        for (int r = p.lane; r < p.rows; r += p.lanes, at += (int64_t)p.lanes * s.vectors) {
+            float f[V], d[V];
+            NormIo<IO>::widen(x[at], f);
+            NormIo<IO>::widen(dy[at], d);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float xh = (f[j] - c.mean[j]) * c.rstd[j], dz = d[j] * slope<ACT>(fmaf(xh, c.gamma[j], c.beta[j]));
+                db[j] += dz;
+                dg[j] = fmaf(dz, xh, dg[j]);
+            }
+        }
+    }
+    const int first = (int)(blockIdx.x % (unsigned)g.pieces) * kThreads, count = min(kThreads, s.vectors - first);
+    if (p.active) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) shared[threadIdx.x * V + j] = make_float2(db[j], dg[j]);
+    }
+    __syncthreads();
+    float2* out = reinterpret_cast<float2*>(g.columns) + (p.b * g.ranges + p.range) * s.D + first * V;
+    for (int c = threadIdx.x; c < count * V; c += kThreads) {
+        float2 all = make_float2(0.0f, 0.0f);
+        for (int l = 0; l < p.lanes; ++l) {
+            const float2 v = shared[l * count * V + c];
+            all.x += v.x; all.y += v.y;
+        }
+        out[c] = all;
+    }
+}
+
+__device__ __forceinline__ float2 warp_sum(float2 v) {
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+        v.x += __shfl_xor_sync(0xffffffffu, v.x, d);
+        v.y += __shfl_xor_sync(0xffffffffu, v.y, d);
+    }
+    return v;
+}
+
+// One CTA an instance and group: a warp adds up a channel, whose tuple and row ranges its lanes share.
+template <typename IO>
+__global__ void __launch_bounds__(kThreads) group_sums_kernel(NormShape s, Ranges g, const IO* gamma, const int32_t* lengths) {
+    ptx::grid_handover();
+    __shared__ float2 shared[kThreads / 32];
+    const int64_t b = blockIdx.x / (unsigned)s.groups;
+    const int group = (int)(blockIdx.x % (unsigned)s.groups), each = s.C / s.groups, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    float2 total = make_float2(0.0f, 0.0f);
+    for (int k = warp; k < each; k += kThreads / 32) {
+        const int channel = group * each + k;
+        const float2* columns = reinterpret_cast<const float2*>(g.columns) + b * g.ranges * s.D + (int64_t)channel * s.T;
+        float2 sum = make_float2(0.0f, 0.0f);
+        for (int64_t i = lane; i < (int64_t)g.ranges * s.T; i += 32) {
+            const float2 v = columns[i / s.T * s.D + i % s.T];
+            sum.x += v.x; sum.y += v.y;
+        }
+        sum = warp_sum(sum);
+        if (lane == 0) reinterpret_cast<float2*>(g.channels)[b * s.C + channel] = sum;
+        const float w = gamma ? NormIo<IO>::one(gamma, channel) : 1.0f;
+        total.x = fmaf(w, sum.x, total.x);
+        total.y = fmaf(w, sum.y, total.y);
+    }
+    if (lane == 0) shared[warp] = total;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kThreads / 32; ++w) { total.x += shared[w].x; total.y += shared[w].y; }
+        const float n = (float)positions_of(lengths, b, s.S) * s.width;
+        reinterpret_cast<float2*>(g.groups)[blockIdx.x] = n > 0.0f ? make_float2(total.x / n, total.y / n) : make_float2(0.0f, 0.0f);
+    }
+}
+
+template <typename IO, int ACT>
+__global__ void __launch_bounds__(kThreads) apply_gradient_kernel(NormShape s, Ranges g, const uint4* x, const uint4* dy, const IO* gamma, const IO* beta,
+                                                                  const int32_t* lengths, const float* stats, uint4* dx) {
+    constexpr int V = NormIo<IO>::kVec;
+    ptx::grid_handover();
+    const Place p = place(s, g, lengths);
+    if (!p.active || p.lane >= p.rows) return;
+    const Column<IO> c(s, reinterpret_cast<const float2*>(stats), gamma, beta, p.b, p.vector);
+    float2 off[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) off[j] = reinterpret_cast<const float2*>(g.groups)[p.b * s.groups + (p.vector * V + j) / s.width];
+    int64_t at = (p.b * s.S + p.row0 + p.lane) * s.vectors + p.vector;
+    for (int r = p.lane; r < p.rows; r += p.lanes, at += (int64_t)p.lanes * s.vectors) {
+        float f[V], d[V];
+        NormIo<IO>::widen(x[at], f);
+        NormIo<IO>::widen(dy[at], d);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const float xh = (f[j] - c.mean[j]) * c.rstd[j], dz = d[j] * slope<ACT>(fmaf(xh, c.gamma[j], c.beta[j]));
+            f[j] = c.rstd[j] * (fmaf(c.gamma[j], dz, -off[j].x) - xh * off[j].y);
+        }
+        dx[at] = NormIo<IO>::narrow(f);
+    }
+}
+
+// dgamma and dbeta: the sum over `parts` rows of float2 [parts][C], eight channels a CTA and 32 chains.
+__global__ void __launch_bounds__(kThreads) parameter_sums_kernel(const float2* parts, int64_t count, int C, float* dgamma, float* dbeta) {
+    ptx::grid_handover();
+    __shared__ float2 shared[kThreads];
+    const int channel = blockIdx.x * 8 + (threadIdx.x & 7);
+    float2 sum = make_float2(0.0f, 0.0f);
+    if (channel < C)
+        for (int64_t i = threadIdx.x >> 3; i < count; i += kThreads / 8) {
+            const float2 v = parts[i * C + channel];
+            sum.x += v.x; sum.y += v.y;
+        }
+    shared[threadIdx.x] = sum;
+    __syncthreads();
+    if (threadIdx.x < 8 && channel < C) {
+        for (int k = 1; k < kThreads / 8; ++k) { sum.x += shared[k * 8 + threadIdx.x].x; sum.y += shared[k * 8 + threadIdx.x].y; }
+        if (dbeta) dbeta[channel] = sum.x;
+        if (dgamma) dgamma[channel] = sum.y;
+    }
+}
+
+inline bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+inline size_t elem(int dtype) { return dtype == EQL_FP32 ? 4 : 2; }
+
+eql_status_t check_norm(const eql_groupnorm_t* n, NormShape* s) {
+    if (!n) return EQL_ERR_INVALID_ARG;
+    if (n->dtype != EQL_FP32 && n->dtype != EQL_FP16 && n->dtype != EQL_BF16) return EQL_ERR_INVALID_ARG;
+    if (n->T < 1 || n->C < 1 || n->groups < 1 || n->C % n->groups != 0) return EQL_ERR_INVALID_ARG;
+    if (n->act < EQL_ACT_NONE || n->act > EQL_ACT_SILU || !(n->eps > 0.0f) || !std::isfinite(n->eps)) return EQL_ERR_INVALID_ARG;
+    if (n->batch < 0 || n->positions < 0) return EQL_ERR_INVALID_ARG;
+    const int64_t most = ((int64_t)1 << 31) - 1024, D = (int64_t)n->C * n->T;
+    if (n->T > 64 || D > (1 << 20) || n->batch > most || n->positions > most || n->batch * n->positions > most) return EQL_ERR_UNSUPPORTED;
+    if (D * elem(n->dtype) % 16 != 0) return EQL_ERR_ALIGNMENT;
+    *s = NormShape{n->T, n->C, n->groups, n->act, (int)D, (int)(D / n->groups), (int)(D * elem(n->dtype) / 16), n->batch, n->positions, n->eps};
+    return EQL_OK;
+}
+
+// Ranges of rows so that a launch fills the device a few times over, of 64 rows at least (the partials are then a small share of the data).
+Ranges make_ranges(const NormShape& s, char* scratch, size_t* bytes) {
+    Ranges g{};
+    g.pieces = (s.vectors + kThreads - 1) / kThreads;
+    const int64_t wanted = (8 * kNumSMs + s.B * g.pieces - 1) / (s.B * g.pieces);
+    const int64_t most = s.S / 64 > 1 ? s.S / 64 : 1;
+    const int64_t ranges = wanted < most ? wanted : most;
+    g.rows = (s.S + ranges - 1) / ranges;
+    g.ranges = (int)((s.S + g.rows - 1) / g.rows);
+    size_t off = 0;
+    g.columns = (float*)(scratch + off);   off += align_up((size_t)s.B * g.ranges * s.D * 8, kWsAlign);
+    g.groups = (float*)(scratch + off);    off += align_up((size_t)s.B * s.groups * 8, kWsAlign);
+    g.channels = (float*)(scratch + off);  off += align_up((size_t)s.B * s.C * 8, kWsAlign);
+    *bytes = off;
+    return g;
+}
+
+template <typename F>
+cudaError_t dispatch_act(int act, F&& f) {
+    if (act == EQL_ACT_GELU) return f(std::integral_constant<int, EQL_ACT_GELU>{});
+    if (act == EQL_ACT_SILU) return f(std::integral_constant<int, EQL_ACT_SILU>{});
+    return f(std::integral_constant<int, EQL_ACT_NONE>{});
+}
+template <typename F>
+cudaError_t dispatch_io(int dtype, F&& f) {
+    if (dtype == EQL_FP16) return f(__half{});
+    if (dtype == EQL_BF16) return f(__nv_bfloat16{});
+    return f(float{});
+}
+
+// Whether [a, a + na) and [b, b + nb) share bytes.
+inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+    const uintptr_t p = (uintptr_t)a, q = (uintptr_t)b;
+    return p < q + nb && q < p + na;
+}
+
+eql_status_t check_scratch(const void* scratch, size_t bytes, size_t need) {
+    if (need == 0) return EQL_OK;
+    if (!scratch) return EQL_ERR_INVALID_ARG;
+    if (!aligned(scratch, kWsAlign)) return EQL_ERR_ALIGNMENT;
+    return bytes < need ? EQL_ERR_WORKSPACE : EQL_OK;
+}
+
+}  // namespace
+}  // namespace eql
+
+using namespace eql;
+
+extern "C" {
+
+eql_status_t eqlinear_groupnorm_scratch_bytes(const eql_groupnorm_t* norm, size_t* bytes) {
+    if (!bytes) return EQL_ERR_INVALID_ARG;
+    NormShape s;
+    if (eql_status_t st = check_norm(norm, &s); st != EQL_OK) return st;
+    *bytes = 0;
+    if (s.B > 0 && s.S > 0) make_ranges(s, nullptr, bytes);
+    return EQL_OK;
+}
+
+eql_status_t eqlinear_groupnorm_fwd(const eql_groupnorm_t* norm, const void* x, const void* gamma, const void* beta, const int32_t* lengths,
+                                    void* y, float* stats, void* scratch, size_t scratch_bytes, void* stream) {
+    NormShape s;
+    if (eql_status_t st = check_norm(norm, &s); st != EQL_OK) return st;
+    if (s.B == 0 || s.S == 0) return EQL_OK;
+    if (!x || !y) return EQL_ERR_INVALID_ARG;
+    if (!aligned(x, 16) || !aligned(y, 16) || !aligned(gamma, 16) || !aligned(beta, 16) || !aligned(lengths, 16) || !aligned(stats, 16))
+        return EQL_ERR_ALIGNMENT;
+    const size_t size = (size_t)s.B * s.S * s.vectors * 16;
+    if (overlap(x, size, y, size)) return EQL_ERR_INVALID_ARG;
+    size_t need = 0;
+    const Ranges g = make_ranges(s, (char*)scratch, &need);
+    if (eql_status_t st = check_scratch(scratch, scratch_bytes, need); st != EQL_OK) return st;
+    const int64_t grid = s.B * g.ranges * g.pieces, units = s.B * s.groups;
+    if (grid > INT32_MAX || units > INT32_MAX) return EQL_ERR_UNSUPPORTED;
+    const cudaStream_t st = (cudaStream_t)stream;
+    const cudaError_t e = dispatch_io(norm->dtype, [&](auto io) {
+        using IO = decltype(io);
+        cudaError_t err = launch_overlapped(column_moments_kernel<IO>, dim3((unsigned)grid), dim3(kThreads), 0, st, s, g, (const uint4*)x, lengths);
+        if (err == cudaSuccess) err = launch_overlapped(group_moments_kernel, dim3((unsigned)units), dim3(kThreads), 0, st, s, g, lengths, stats);
+        if (err != cudaSuccess) return err;
+        return dispatch_act(s.act, [&](auto act) {
+            return launch_overlapped(apply_kernel<IO, decltype(act)::value>, dim3((unsigned)grid), dim3(kThreads), 0, st, s, g, (const uint4*)x,
+                                     (const IO*)gamma, (const IO*)beta, lengths, (uint4*)y);
+        });
+    });
+    return e == cudaSuccess ? EQL_OK : EQL_ERR_CUDA;
+}
+
+eql_status_t eqlinear_groupnorm_bwd(const eql_groupnorm_t* norm, const void* x, const void* dy, const void* gamma, const void* beta,
+                                    const int32_t* lengths, const float* stats, void* dx, void* dgamma, void* dbeta,
+                                    void* scratch, size_t scratch_bytes, void* stream) {
+    NormShape s;
+    if (eql_status_t st = check_norm(norm, &s); st != EQL_OK) return st;
+    if (!aligned(dgamma, 16) || !aligned(dbeta, 16)) return EQL_ERR_ALIGNMENT;
+    const cudaStream_t st = (cudaStream_t)stream;
+    if (s.B == 0 || s.S == 0) {
+        if (dgamma && cudaMemsetAsync(dgamma, 0, s.C * sizeof(float), st) != cudaSuccess) return EQL_ERR_CUDA;
+        if (dbeta && cudaMemsetAsync(dbeta, 0, s.C * sizeof(float), st) != cudaSuccess) return EQL_ERR_CUDA;
+        return EQL_OK;
+    }
+    if (!x || !dy || !stats || !dx) return EQL_ERR_INVALID_ARG;
+    if (!aligned(x, 16) || !aligned(dy, 16) || !aligned(dx, 16) || !aligned(gamma, 16) || !aligned(beta, 16) || !aligned(lengths, 16) ||
+        !aligned(stats, 16))
+        return EQL_ERR_ALIGNMENT;
+    const size_t size = (size_t)s.B * s.S * s.vectors * 16;
+    if (overlap(x, size, dx, size) || overlap(dy, size, dx, size)) return EQL_ERR_INVALID_ARG;
+    size_t need = 0;
+    const Ranges g = make_ranges(s, (char*)scratch, &need);
+    if (eql_status_t e = check_scratch(scratch, scratch_bytes, need); e != EQL_OK) return e;
+    const int64_t grid = s.B * g.ranges * g.pieces, units = s.B * s.groups;
+    if (grid > INT32_MAX || units > INT32_MAX) return EQL_ERR_UNSUPPORTED;
+    const cudaError_t e = dispatch_io(norm->dtype, [&](auto io) {
+        using IO = decltype(io);
+        return dispatch_act(s.act, [&](auto act) {
+            constexpr int ACT = decltype(act)::value;
+            cudaError_t err = launch_overlapped(column_sums_kernel<IO, ACT>, dim3((unsigned)grid), dim3(kThreads), 0, st, s, g, (const uint4*)x,
+                                                (const uint4*)dy, (const IO*)gamma, (const IO*)beta, lengths, stats);
+            if (err == cudaSuccess)
+                err = launch_overlapped(group_sums_kernel<IO>, dim3((unsigned)units), dim3(kThreads), 0, st, s, g, (const IO*)gamma, lengths);
+            if (err == cudaSuccess)
+                err = launch_overlapped(apply_gradient_kernel<IO, ACT>, dim3((unsigned)grid), dim3(kThreads), 0, st, s, g, (const uint4*)x,
+                                        (const uint4*)dy, (const IO*)gamma, (const IO*)beta, lengths, stats, (uint4*)dx);
+            if (err == cudaSuccess && (dgamma || dbeta))
+                err = launch_overlapped(parameter_sums_kernel, dim3((unsigned)((s.C + 7) / 8)), dim3(kThreads), 0, st, (const float2*)g.channels, s.B,
+                                        s.C, (float*)dgamma, (float*)dbeta);
+            return err;
+        });
+    });
+    return e == cudaSuccess ? EQL_OK : EQL_ERR_CUDA;
+}
+
+}  // extern "C"
