@@ -285,7 +285,7 @@ eql_status_t check_norm(const eql_groupnorm_t* n, NormShape* s) {
 }
 
 // Ranges of rows so that a launch fills the device a few times over, of 64 rows at least (the partials are then a small share of the data).
-Ranges make_ranges(const NormShape& s, char* scratch, size_t* bytes) {
+Ranges range_plan(const NormShape& s, char* scratch, size_t* bytes) {
     Ranges g{};
     g.pieces = (s.vectors + kThreads - 1) / kThreads;
     const int64_t wanted = (8 * kNumSMs + s.B * g.pieces - 1) / (s.B * g.pieces);
@@ -301,17 +301,63 @@ Ranges make_ranges(const NormShape& s, char* scratch, size_t* bytes) {
     return g;
 }
 
-template <typename F>
-cudaError_t dispatch_act(int act, F&& f) {
-    if (act == EQL_ACT_GELU) return f(std::integral_constant<int, EQL_ACT_GELU>{});
-    if (act == EQL_ACT_SILU) return f(std::integral_constant<int, EQL_ACT_SILU>{});
-    return f(std::integral_constant<int, EQL_ACT_NONE>{});
+// How one direction of a norm runs, by its shape alone.
+struct NormPlan {
+    WarpNorm warp;
+    Ranges ranges;            // where no other kernel takes the shape
+    size_t scratch_bytes;
+    bool fits;                // its launches
+};
+NormPlan norm_plan(const NormShape& s, eql_dtype_t dtype, bool backward, char* scratch) {
+    NormPlan p{};
+    p.fits = true;
+    p.warp = warp_norm_plan(s, dtype, backward);
+    if (p.warp.supported) {
+        p.scratch_bytes = backward ? align_up((size_t)p.warp.ctas * s.C * 8, kWsAlign) : 0;
+        return p;
+    }
+    p.ranges = range_plan(s, scratch, &p.scratch_bytes);
+    p.fits = s.B * p.ranges.ranges * p.ranges.pieces <= INT32_MAX && s.B * s.groups <= INT32_MAX;
+    return p;
 }
-template <typename F>
-cudaError_t dispatch_io(int dtype, F&& f) {
-    if (dtype == EQL_FP16) return f(__half{});
-    if (dtype == EQL_BF16) return f(__nv_bfloat16{});
-    return f(float{});
+
+cudaError_t launch_parameter_sums(const float* parts, int64_t count, int C, float* dgamma, float* dbeta, cudaStream_t stream) {
+    if (!dgamma && !dbeta) return cudaSuccess;
+    return launch_overlapped(parameter_sums_kernel, dim3((unsigned)((C + 7) / 8)), dim3(kThreads), 0, stream, (const float2*)parts, count, C, dgamma, dbeta);
+}
+
+cudaError_t run_ranges(const NormShape& s, const Ranges& g, eql_dtype_t dtype, const void* x, const void* gamma, const void* beta, const int32_t* lengths,
+                       void* y, float* stats, cudaStream_t st) {
+    const int64_t grid = s.B * g.ranges * g.pieces, units = s.B * s.groups;
+    return dispatch_io(dtype, [&](auto io) {
+        using IO = decltype(io);
+        cudaError_t err = launch_overlapped(column_moments_kernel<IO>, dim3((unsigned)grid), dim3(kThreads), 0, st, s, g, (const uint4*)x, lengths);
+        if (err == cudaSuccess) err = launch_overlapped(group_moments_kernel, dim3((unsigned)units), dim3(kThreads), 0, st, s, g, lengths, stats);
+        if (err != cudaSuccess) return err;
+        return dispatch_act(s.act, [&](auto act) {
+            return launch_overlapped(apply_kernel<IO, decltype(act)::value>, dim3((unsigned)grid), dim3(kThreads), 0, st, s, g, (const uint4*)x,
+                                     (const IO*)gamma, (const IO*)beta, lengths, (uint4*)y);
+        });
+    });
+}
+
+cudaError_t run_ranges_gradient(const NormShape& s, const Ranges& g, eql_dtype_t dtype, const void* x, const void* dy, const void* gamma, const void* beta,
+                                const int32_t* lengths, const float* stats, void* dx, float* dgamma, float* dbeta, cudaStream_t st) {
+    const int64_t grid = s.B * g.ranges * g.pieces, units = s.B * s.groups;
+    return dispatch_io(dtype, [&](auto io) {
+        using IO = decltype(io);
+        return dispatch_act(s.act, [&](auto act) {
+            constexpr int ACT = decltype(act)::value;
+            cudaError_t err = launch_overlapped(column_sums_kernel<IO, ACT>, dim3((unsigned)grid), dim3(kThreads), 0, st, s, g, (const uint4*)x,
+                                                (const uint4*)dy, (const IO*)gamma, (const IO*)beta, lengths, stats);
+            if (err == cudaSuccess)
+                err = launch_overlapped(group_sums_kernel<IO>, dim3((unsigned)units), dim3(kThreads), 0, st, s, g, (const IO*)gamma, lengths);
+            if (err == cudaSuccess)
+                err = launch_overlapped(apply_gradient_kernel<IO, ACT>, dim3((unsigned)grid), dim3(kThreads), 0, st, s, g, (const uint4*)x,
+                                        (const uint4*)dy, (const IO*)gamma, (const IO*)beta, lengths, stats, (uint4*)dx);
+            return err == cudaSuccess ? launch_parameter_sums(g.channels, s.B, s.C, dgamma, dbeta, st) : err;
+        });
+    });
 }
 
 // Whether [a, a + na) and [b, b + nb) share bytes.
@@ -339,7 +385,11 @@ eql_status_t eqlinear_groupnorm_scratch_bytes(const eql_groupnorm_t* norm, size_
     NormShape s;
     if (eql_status_t st = check_norm(norm, &s); st != EQL_OK) return st;
     *bytes = 0;
-    if (s.B > 0 && s.S > 0) make_ranges(s, nullptr, bytes);
+    if (s.B > 0 && s.S > 0) {
+        const eql_dtype_t dtype = (eql_dtype_t)norm->dtype;
+        const size_t fwd = norm_plan(s, dtype, false, nullptr).scratch_bytes, bwd = norm_plan(s, dtype, true, nullptr).scratch_bytes;
+        *bytes = fwd > bwd ? fwd : bwd;
+    }
     return EQL_OK;
 }
 
@@ -353,22 +403,13 @@ eql_status_t eqlinear_groupnorm_fwd(const eql_groupnorm_t* norm, const void* x, 
         return EQL_ERR_ALIGNMENT;
     const size_t size = (size_t)s.B * s.S * s.vectors * 16;
     if (overlap(x, size, y, size)) return EQL_ERR_INVALID_ARG;
-    size_t need = 0;
-    const Ranges g = make_ranges(s, (char*)scratch, &need);
-    if (eql_status_t st = check_scratch(scratch, scratch_bytes, need); st != EQL_OK) return st;
-    const int64_t grid = s.B * g.ranges * g.pieces, units = s.B * s.groups;
-    if (grid > INT32_MAX || units > INT32_MAX) return EQL_ERR_UNSUPPORTED;
+    const eql_dtype_t dtype = (eql_dtype_t)norm->dtype;
+    const NormPlan p = norm_plan(s, dtype, false, (char*)scratch);
+    if (!p.fits) return EQL_ERR_UNSUPPORTED;
+    if (eql_status_t st = check_scratch(scratch, scratch_bytes, p.scratch_bytes); st != EQL_OK) return st;
     const cudaStream_t st = (cudaStream_t)stream;
-    const cudaError_t e = dispatch_io(norm->dtype, [&](auto io) {
-        using IO = decltype(io);
-        cudaError_t err = launch_overlapped(column_moments_kernel<IO>, dim3((unsigned)grid), dim3(kThreads), 0, st, s, g, (const uint4*)x, lengths);
-        if (err == cudaSuccess) err = launch_overlapped(group_moments_kernel, dim3((unsigned)units), dim3(kThreads), 0, st, s, g, lengths, stats);
-        if (err != cudaSuccess) return err;
-        return dispatch_act(s.act, [&](auto act) {
-            return launch_overlapped(apply_kernel<IO, decltype(act)::value>, dim3((unsigned)grid), dim3(kThreads), 0, st, s, g, (const uint4*)x,
-                                     (const IO*)gamma, (const IO*)beta, lengths, (uint4*)y);
-        });
-    });
+    const cudaError_t e = p.warp.supported ? launch_warp_norm(s, p.warp, dtype, x, gamma, beta, lengths, y, stats, st)
+                                           : run_ranges(s, p.ranges, dtype, x, gamma, beta, lengths, y, stats, st);
     return e == cudaSuccess ? EQL_OK : EQL_ERR_CUDA;
 }
 
@@ -390,28 +431,17 @@ eql_status_t eqlinear_groupnorm_bwd(const eql_groupnorm_t* norm, const void* x, 
         return EQL_ERR_ALIGNMENT;
     const size_t size = (size_t)s.B * s.S * s.vectors * 16;
     if (overlap(x, size, dx, size) || overlap(dy, size, dx, size)) return EQL_ERR_INVALID_ARG;
-    size_t need = 0;
-    const Ranges g = make_ranges(s, (char*)scratch, &need);
-    if (eql_status_t e = check_scratch(scratch, scratch_bytes, need); e != EQL_OK) return e;
-    const int64_t grid = s.B * g.ranges * g.pieces, units = s.B * s.groups;
-    if (grid > INT32_MAX || units > INT32_MAX) return EQL_ERR_UNSUPPORTED;
-    const cudaError_t e = dispatch_io(norm->dtype, [&](auto io) {
-        using IO = decltype(io);
-        return dispatch_act(s.act, [&](auto act) {
-            constexpr int ACT = decltype(act)::value;
-            cudaError_t err = launch_overlapped(column_sums_kernel<IO, ACT>, dim3((unsigned)grid), dim3(kThreads), 0, st, s, g, (const uint4*)x,
-                                                (const uint4*)dy, (const IO*)gamma, (const IO*)beta, lengths, stats);
-            if (err == cudaSuccess)
-                err = launch_overlapped(group_sums_kernel<IO>, dim3((unsigned)units), dim3(kThreads), 0, st, s, g, (const IO*)gamma, lengths);
-            if (err == cudaSuccess)
-                err = launch_overlapped(apply_gradient_kernel<IO, ACT>, dim3((unsigned)grid), dim3(kThreads), 0, st, s, g, (const uint4*)x,
-                                        (const uint4*)dy, (const IO*)gamma, (const IO*)beta, lengths, stats, (uint4*)dx);
-            if (err == cudaSuccess && (dgamma || dbeta))
-                err = launch_overlapped(parameter_sums_kernel, dim3((unsigned)((s.C + 7) / 8)), dim3(kThreads), 0, st, (const float2*)g.channels, s.B,
-                                        s.C, (float*)dgamma, (float*)dbeta);
-            return err;
-        });
-    });
+    const eql_dtype_t dtype = (eql_dtype_t)norm->dtype;
+    const NormPlan p = norm_plan(s, dtype, true, (char*)scratch);
+    if (!p.fits) return EQL_ERR_UNSUPPORTED;
+    if (eql_status_t e = check_scratch(scratch, scratch_bytes, p.scratch_bytes); e != EQL_OK) return e;
+    cudaError_t e;
+    if (p.warp.supported) {
+        e = launch_warp_gradient(s, p.warp, dtype, x, dy, gamma, beta, lengths, stats, dx, (float*)scratch, st);
+        if (e == cudaSuccess) e = launch_parameter_sums((const float*)scratch, p.warp.ctas, s.C, (float*)dgamma, (float*)dbeta, st);
+    } else {
+        e = run_ranges_gradient(s, p.ranges, dtype, x, dy, gamma, beta, lengths, stats, dx, (float*)dgamma, (float*)dbeta, st);
+    }
     return e == cudaSuccess ? EQL_OK : EQL_ERR_CUDA;
 }
 

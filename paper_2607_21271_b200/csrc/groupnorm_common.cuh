@@ -7,6 +7,9 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <climits>
+#include <type_traits>
+
 #include "eql_internal.h"
 #include "ptx_sm100.cuh"
 
@@ -20,6 +23,36 @@ struct NormShape {
     int64_t B, S;
     float eps;
 };
+
+// Small units (groupnorm_warp.cu): a unit is one instance's part of one group.
+struct WarpNorm {
+    bool supported;
+    int vectors, unit;        // 16-byte vectors of a row of the unit, and of the unit
+    int lanes, each;          // lanes a unit has, vectors a lane (rounded up to what kernels exist for)
+    int groups, instances;    // units that a CTA holds at a time: so many groups of so many instances
+    int group_blocks, ctas;   // CTAs that cover all groups, and how many such sets there are
+    int sums, shared_bytes;
+};
+constexpr int kWarpNormShared = 66 * 1024;        // 256 lanes x 4 vectors x 8 sums x 8 bytes, and some
+WarpNorm warp_norm_plan(const NormShape& s, eql_dtype_t dtype, bool backward);
+cudaError_t launch_warp_norm(const NormShape& s, const WarpNorm& w, eql_dtype_t dtype, const void* x, const void* gamma, const void* beta,
+                             const int32_t* lengths, void* y, float* stats, cudaStream_t stream);
+// parts: float2 [ctas][C], the CTAs' sums of dz and dz * xh
+cudaError_t launch_warp_gradient(const NormShape& s, const WarpNorm& w, eql_dtype_t dtype, const void* x, const void* dy, const void* gamma,
+                                 const void* beta, const int32_t* lengths, const float* stats, void* dx, float* parts, cudaStream_t stream);
+
+template <typename F>
+cudaError_t dispatch_act(int act, F&& f) {
+    if (act == EQL_ACT_GELU) return f(std::integral_constant<int, EQL_ACT_GELU>{});
+    if (act == EQL_ACT_SILU) return f(std::integral_constant<int, EQL_ACT_SILU>{});
+    return f(std::integral_constant<int, EQL_ACT_NONE>{});
+}
+template <typename F>
+cudaError_t dispatch_io(int dtype, F&& f) {
+    if (dtype == EQL_FP16) return f(__half{});
+    if (dtype == EQL_BF16) return f(__nv_bfloat16{});
+    return f(float{});
+}
 
 template <typename IO> struct NormIo;
 template <> struct NormIo<float> {
