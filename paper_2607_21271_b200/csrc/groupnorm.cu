@@ -52,11 +52,11 @@ __global__ void __launch_bounds__(kThreads) column_moments_kernel(NormShape s, R
     ptx::grid_handover();
     __shared__ float2 shared[kThreads * V];
     const Place p = place(s, g, lengths);
-    RunningMoments<V> m;
+    RunningMoments<V / 2> m;
     if (p.active) {
         const uint4* at = x + (p.b * s.S + p.row0 + p.lane) * s.vectors + p.vector;
         for (int r = p.lane; r < p.rows; r += p.lanes, at += (int64_t)p.lanes * s.vectors) {
-            float f[V];
+            float2 f[V / 2];
             NormIo<IO>::widen(*at, f);
             m.add(f);
         }
@@ -65,7 +65,10 @@ __global__ void __launch_bounds__(kThreads) column_moments_kernel(NormShape s, R
     auto rows_of = [&](int lane) { return (float)((p.rows - lane + p.lanes - 1) / p.lanes); };
     if (p.active) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) shared[threadIdx.x * V + j] = make_float2(m.mean[j], m.m2[j]);
+        for (int j = 0; j < V / 2; ++j) {
+            shared[threadIdx.x * V + 2 * j] = make_float2(m.mean[j].x, m.m2[j].x);
+            shared[threadIdx.x * V + 2 * j + 1] = make_float2(m.mean[j].y, m.m2[j].y);
+        }
     }
     __syncthreads();
     const int first = (int)(blockIdx.x % (unsigned)g.pieces) * kThreads * V;
@@ -110,15 +113,16 @@ __global__ void __launch_bounds__(kThreads) group_moments_kernel(NormShape s, Ra
 template <typename IO>
 struct Column {
     static constexpr int V = NormIo<IO>::kVec;
-    float mean[V], rstd[V], gamma[V], beta[V];
+    float2 mean[V / 2], rstd[V / 2], gamma[V / 2], beta[V / 2];
     __device__ __forceinline__ Column(const NormShape& s, const float2* stats, const IO* gammas, const IO* betas, int64_t b, int vector) {
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const int e = vector * V + j, channel = e / s.T;
             const float2 st = stats[b * s.groups + e / s.width];
-            mean[j] = st.x; rstd[j] = st.y;
-            gamma[j] = gammas ? NormIo<IO>::one(gammas, channel) : 1.0f;
-            beta[j] = betas ? NormIo<IO>::one(betas, channel) : 0.0f;
+            (&mean[j / 2].x)[j % 2] = st.x;
+            (&rstd[j / 2].x)[j % 2] = st.y;
+            (&gamma[j / 2].x)[j % 2] = gammas ? NormIo<IO>::one(gammas, channel) : 1.0f;
+            (&beta[j / 2].x)[j % 2] = betas ? NormIo<IO>::one(betas, channel) : 0.0f;
         }
     }
 };
@@ -132,13 +136,13 @@ __global__ void __launch_bounds__(kThreads) apply_kernel(NormShape s, Ranges g, 
     if (!p.active || p.lane >= p.rows) return;
     Column<IO> c(s, reinterpret_cast<const float2*>(g.groups), gamma, beta, p.b, p.vector);
 #pragma unroll
-    for (int j = 0; j < V; ++j) c.gamma[j] *= c.rstd[j];
+    for (int j = 0; j < V / 2; ++j) c.gamma[j] = mul2(c.gamma[j], c.rstd[j]);
     int64_t at = (p.b * s.S + p.row0 + p.lane) * s.vectors + p.vector;
     for (int r = p.lane; r < p.rows; r += p.lanes, at += (int64_t)p.lanes * s.vectors) {
-        float f[V];
+        float2 f[V / 2];
         NormIo<IO>::widen(x[at], f);
 #pragma unroll
-        for (int j = 0; j < V; ++j) f[j] = activate<ACT>(fmaf(f[j] - c.mean[j], c.gamma[j], c.beta[j]));
+        for (int j = 0; j < V / 2; ++j) f[j] = activate<ACT>(fma2(sub2(f[j], c.mean[j]), c.gamma[j], c.beta[j]));
         y[at] = NormIo<IO>::narrow(f);
     }
 }
@@ -150,26 +154,29 @@ __global__ void __launch_bounds__(kThreads) column_sums_kernel(NormShape s, Rang
     ptx::grid_handover();
     __shared__ float2 shared[kThreads * V];
     const Place p = place(s, g, lengths);
-    float db[V] = {}, dg[V] = {};
+    float2 db[V / 2] = {}, dg[V / 2] = {};
     if (p.active && p.lane < p.rows) {
         const Column<IO> c(s, reinterpret_cast<const float2*>(stats), gamma, beta, p.b, p.vector);
         int64_t at = (p.b * s.S + p.row0 + p.lane) * s.vectors + p.vector;
         for (int r = p.lane; r < p.rows; r += p.lanes, at += (int64_t)p.lanes * s.vectors) {
-            float f[V], d[V];
+            float2 f[V / 2], d[V / 2];
             NormIo<IO>::widen(x[at], f);
             NormIo<IO>::widen(dy[at], d);
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const float xh = (f[j] - c.mean[j]) * c.rstd[j], dz = d[j] * slope<ACT>(fmaf(xh, c.gamma[j], c.beta[j]));
-                db[j] += dz;
-                dg[j] = fmaf(dz, xh, dg[j]);
+            for (int j = 0; j < V / 2; ++j) {
+                const float2 xh = mul2(sub2(f[j], c.mean[j]), c.rstd[j]), dz = mul2(d[j], slope<ACT>(fma2(xh, c.gamma[j], c.beta[j])));
+                db[j] = add2(db[j], dz);
+                dg[j] = fma2(dz, xh, dg[j]);
             }
         }
     }
     const int first = (int)(blockIdx.x % (unsigned)g.pieces) * kThreads, count = min(kThreads, s.vectors - first);
     if (p.active) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) shared[threadIdx.x * V + j] = make_float2(db[j], dg[j]);
+        for (int j = 0; j < V / 2; ++j) {
+            shared[threadIdx.x * V + 2 * j] = make_float2(db[j].x, dg[j].x);
+            shared[threadIdx.x * V + 2 * j + 1] = make_float2(db[j].y, dg[j].y);
+        }
     }
     __syncthreads();
     float2* out = reinterpret_cast<float2*>(g.columns) + (p.b * g.ranges + p.range) * s.D + first * V;
@@ -231,18 +238,22 @@ __global__ void __launch_bounds__(kThreads) apply_gradient_kernel(NormShape s, R
     const Place p = place(s, g, lengths);
     if (!p.active || p.lane >= p.rows) return;
     const Column<IO> c(s, reinterpret_cast<const float2*>(stats), gamma, beta, p.b, p.vector);
-    float2 off[V];
+    float2 off1[V / 2], off2[V / 2];
 #pragma unroll
-    for (int j = 0; j < V; ++j) off[j] = reinterpret_cast<const float2*>(g.groups)[p.b * s.groups + (p.vector * V + j) / s.width];
+    for (int j = 0; j < V; ++j) {
+        const float2 v = reinterpret_cast<const float2*>(g.groups)[p.b * s.groups + (p.vector * V + j) / s.width];
+        (&off1[j / 2].x)[j % 2] = -v.x;
+        (&off2[j / 2].x)[j % 2] = -v.y;
+    }
     int64_t at = (p.b * s.S + p.row0 + p.lane) * s.vectors + p.vector;
     for (int r = p.lane; r < p.rows; r += p.lanes, at += (int64_t)p.lanes * s.vectors) {
-        float f[V], d[V];
+        float2 f[V / 2], d[V / 2];
         NormIo<IO>::widen(x[at], f);
         NormIo<IO>::widen(dy[at], d);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const float xh = (f[j] - c.mean[j]) * c.rstd[j], dz = d[j] * slope<ACT>(fmaf(xh, c.gamma[j], c.beta[j]));
-            f[j] = c.rstd[j] * (fmaf(c.gamma[j], dz, -off[j].x) - xh * off[j].y);
+        for (int j = 0; j < V / 2; ++j) {
+            const float2 xh = mul2(sub2(f[j], c.mean[j]), c.rstd[j]), dz = mul2(d[j], slope<ACT>(fma2(xh, c.gamma[j], c.beta[j])));
+            f[j] = mul2(c.rstd[j], fma2(xh, off2[j], fma2(c.gamma[j], dz, off1[j])));
         }
         dx[at] = NormIo<IO>::narrow(f);
     }
@@ -304,6 +315,7 @@ Ranges range_plan(const NormShape& s, char* scratch, size_t* bytes) {
 // How one direction of a norm runs, by its shape alone.
 struct NormPlan {
     WarpNorm warp;
+    ResidentNorm resident;
     Ranges ranges;            // where no other kernel takes the shape
     size_t scratch_bytes;
     bool fits;                // its launches
@@ -314,6 +326,11 @@ NormPlan norm_plan(const NormShape& s, eql_dtype_t dtype, bool backward, char* s
     p.warp = warp_norm_plan(s, dtype, backward);
     if (p.warp.supported) {
         p.scratch_bytes = backward ? align_up((size_t)p.warp.ctas * s.C * 8, kWsAlign) : 0;
+        return p;
+    }
+    p.resident = resident_norm_plan(s, dtype, backward);
+    if (p.resident.supported) {
+        p.scratch_bytes = backward ? align_up((size_t)s.B * p.resident.cluster * s.C * 8, kWsAlign) : 0;
         return p;
     }
     p.ranges = range_plan(s, scratch, &p.scratch_bytes);
@@ -409,7 +426,8 @@ eql_status_t eqlinear_groupnorm_fwd(const eql_groupnorm_t* norm, const void* x, 
     if (eql_status_t st = check_scratch(scratch, scratch_bytes, p.scratch_bytes); st != EQL_OK) return st;
     const cudaStream_t st = (cudaStream_t)stream;
     const cudaError_t e = p.warp.supported ? launch_warp_norm(s, p.warp, dtype, x, gamma, beta, lengths, y, stats, st)
-                                           : run_ranges(s, p.ranges, dtype, x, gamma, beta, lengths, y, stats, st);
+                          : p.resident.supported ? launch_resident_norm(s, p.resident, dtype, x, gamma, beta, lengths, y, stats, st)
+                                                 : run_ranges(s, p.ranges, dtype, x, gamma, beta, lengths, y, stats, st);
     return e == cudaSuccess ? EQL_OK : EQL_ERR_CUDA;
 }
 
@@ -439,6 +457,10 @@ eql_status_t eqlinear_groupnorm_bwd(const eql_groupnorm_t* norm, const void* x, 
     if (p.warp.supported) {
         e = launch_warp_gradient(s, p.warp, dtype, x, dy, gamma, beta, lengths, stats, dx, (float*)scratch, st);
         if (e == cudaSuccess) e = launch_parameter_sums((const float*)scratch, p.warp.ctas, s.C, (float*)dgamma, (float*)dbeta, st);
+    } else if (p.resident.supported) {
+        e = launch_resident_gradient(s, p.resident, dtype, x, dy, gamma, beta, lengths, stats, dx, (float*)scratch, st);
+        if (e == cudaSuccess)
+            e = launch_parameter_sums((const float*)scratch, s.B * p.resident.cluster, s.C, (float*)dgamma, (float*)dbeta, st);
     } else {
         e = run_ranges_gradient(s, p.ranges, dtype, x, dy, gamma, beta, lengths, stats, dx, (float*)dgamma, (float*)dbeta, st);
     }

@@ -41,6 +41,23 @@ cudaError_t launch_warp_norm(const NormShape& s, const WarpNorm& w, eql_dtype_t 
 cudaError_t launch_warp_gradient(const NormShape& s, const WarpNorm& w, eql_dtype_t dtype, const void* x, const void* dy, const void* gamma,
                                  const void* beta, const int32_t* lengths, const float* stats, void* dx, float* parts, cudaStream_t stream);
 
+// Units resident in shared memory (groupnorm_resident.cu): a unit is one instance's part of a block of groups.
+struct ResidentNorm {
+    bool supported;
+    int groups, blocks;       // groups of a block, blocks of a row
+    int cluster, threads;     // CTAs of a unit, threads of a CTA
+    int64_t rows;             // rows of a CTA
+    int run, sums, share;     // backward: neighbouring elements summed up in a thread, sums of a vector, lanes that add up a channel
+    int slot_bytes, side_offset, shared_bytes;
+};
+constexpr int kResidentShared = 220 * 1024;
+ResidentNorm resident_norm_plan(const NormShape& s, eql_dtype_t dtype, bool backward);
+cudaError_t launch_resident_norm(const NormShape& s, const ResidentNorm& r, eql_dtype_t dtype, const void* x, const void* gamma, const void* beta,
+                                 const int32_t* lengths, void* y, float* stats, cudaStream_t stream);
+// parts: float2 [B * cluster][C], the CTAs' sums of dz and dz * xh
+cudaError_t launch_resident_gradient(const NormShape& s, const ResidentNorm& r, eql_dtype_t dtype, const void* x, const void* dy, const void* gamma,
+                                     const void* beta, const int32_t* lengths, const float* stats, void* dx, float* parts, cudaStream_t stream);
+
 template <typename F>
 cudaError_t dispatch_act(int act, F&& f) {
     if (act == EQL_ACT_GELU) return f(std::integral_constant<int, EQL_ACT_GELU>{});
@@ -54,32 +71,50 @@ cudaError_t dispatch_io(int dtype, F&& f) {
     return f(float{});
 }
 
+// Two floats as one operand: a packed operation takes one issue slot, of which these kernels run out before anything else but the memory.
+__device__ __forceinline__ float2 pair(float v) { return make_float2(v, v); }
+#define EQL_PACKED(name, op)                                                                                                     \
+    __device__ __forceinline__ float2 name(float2 a, float2 b) {                                                                 \
+        float2 d;                                                                                                                \
+        asm(op ".rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t&>(d)) : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b))); \
+        return d;                                                                                                                \
+    }
+EQL_PACKED(add2, "add")
+EQL_PACKED(mul2, "mul")
+#undef EQL_PACKED
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(reinterpret_cast<uint64_t&>(d)) : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)),
+        "l"(reinterpret_cast<uint64_t&>(c)));
+    return d;
+}
+__device__ __forceinline__ float2 sub2(float2 a, float2 b) { return fma2(b, pair(-1.0f), a); }
+
+// A vector of 16 bytes as pairs of floats.
 template <typename IO> struct NormIo;
 template <> struct NormIo<float> {
     static constexpr int kVec = 4;
-    static __device__ __forceinline__ void widen(const uint4& u, float* f) {
-        f[0] = __uint_as_float(u.x); f[1] = __uint_as_float(u.y); f[2] = __uint_as_float(u.z); f[3] = __uint_as_float(u.w);
+    static __device__ __forceinline__ void widen(const uint4& u, float2* f) {
+        f[0] = make_float2(__uint_as_float(u.x), __uint_as_float(u.y));
+        f[1] = make_float2(__uint_as_float(u.z), __uint_as_float(u.w));
     }
-    static __device__ __forceinline__ uint4 narrow(const float* f) {
-        return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    static __device__ __forceinline__ uint4 narrow(const float2* f) {
+        return make_uint4(__float_as_uint(f[0].x), __float_as_uint(f[0].y), __float_as_uint(f[1].x), __float_as_uint(f[1].y));
     }
     static __device__ __forceinline__ float one(const float* p, int i) { return p[i]; }
 };
 template <> struct NormIo<__half> {
     static constexpr int kVec = 8;
-    static __device__ __forceinline__ void widen(const uint4& u, float* f) {
+    static __device__ __forceinline__ void widen(const uint4& u, float2* f) {
         const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-            f[2 * i] = p.x; f[2 * i + 1] = p.y;
-        }
+        for (int i = 0; i < 4; ++i) f[i] = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
     }
-    static __device__ __forceinline__ uint4 narrow(const float* f) {
+    static __device__ __forceinline__ uint4 narrow(const float2* f) {
         uint32_t w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const __half2 h = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+            const __half2 h = __floats2half2_rn(f[i].x, f[i].y);
             w[i] = *reinterpret_cast<const uint32_t*>(&h);
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
@@ -88,19 +123,16 @@ template <> struct NormIo<__half> {
 };
 template <> struct NormIo<__nv_bfloat16> {
     static constexpr int kVec = 8;
-    static __device__ __forceinline__ void widen(const uint4& u, float* f) {
+    static __device__ __forceinline__ void widen(const uint4& u, float2* f) {
         const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            f[2 * i] = __uint_as_float(w[i] << 16);
-            f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        }
+        for (int i = 0; i < 4; ++i) f[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
     }
-    static __device__ __forceinline__ uint4 narrow(const float* f) {
+    static __device__ __forceinline__ uint4 narrow(const float2* f) {
         uint32_t w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+            const __nv_bfloat162 h = __floats2bfloat162_rn(f[i].x, f[i].y);
             w[i] = *reinterpret_cast<const uint32_t*>(&h);
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
@@ -128,19 +160,20 @@ __device__ __forceinline__ Moments warp_merge(Moments v) {
     }
     return v;                 // lane 0's
 }
-// The running form (Welford 1962) for columns of V values, row after row: a fourth operation an element, and unlike with sums behind a
+// The running form (Welford 1962) for columns of 2 P values, row after row: a fourth operation an element, and unlike with sums behind a
 // fixed pivot it does not matter how far the first value lies from the rest.
-template <int V>
+template <int P>
 struct RunningMoments {
-    float rows = 0.0f, mean[V] = {}, m2[V] = {};
-    __device__ __forceinline__ void add(const float* f) {
+    float rows = 0.0f;
+    float2 mean[P] = {}, m2[P] = {};
+    __device__ __forceinline__ void add(const float2* f) {
         rows += 1.0f;
-        const float share = __fdividef(1.0f, rows);
+        const float2 share = pair(__fdividef(1.0f, rows));
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const float d = f[j] - mean[j];
-            mean[j] = fmaf(d, share, mean[j]);
-            m2[j] = fmaf(d, f[j] - mean[j], m2[j]);
+        for (int j = 0; j < P; ++j) {
+            const float2 d = sub2(f[j], mean[j]);
+            mean[j] = fma2(d, share, mean[j]);
+            m2[j] = fma2(d, sub2(f[j], mean[j]), m2[j]);
         }
     }
 };
@@ -152,19 +185,59 @@ __device__ __forceinline__ int64_t positions_of(const int32_t* lengths, int64_t 
     return n < 0 ? 0 : n > S ? S : n;
 }
 
-template <int ACT> __device__ __forceinline__ float activate(float z) {
-    if (ACT == EQL_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752440f));
-    if (ACT == EQL_ACT_SILU) return __fdividef(z, 1.0f + __expf(-z));
+__device__ __forceinline__ float exp2_fast(float v) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float reciprocal(float v) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float2 exp2_fast(float2 v) { return make_float2(exp2_fast(v.x), exp2_fast(v.y)); }
+__device__ __forceinline__ float2 reciprocal(float2 v) { return make_float2(reciprocal(v.x), reciprocal(v.y)); }
+
+__device__ __forceinline__ float2 minus_abs(float2 v) { return make_float2(-fabsf(v.x), -fabsf(v.y)); }
+
+// 1 / (1 + exp(-z)): two special-function operations good to 2^-22; 0 where exp(-z) is beyond float.
+__device__ __forceinline__ float2 sigmoid(float2 z) {
+    return reciprocal(add2(exp2_fast(mul2(z, pair(-1.44269504088896341f))), pair(1.0f)));
+}
+// Phi(-|z|) = erfc(|z| / sqrt 2) / 2 by the rational approximation 7.1.26 of Abramowitz and Stegun (error of erfc at most 1.5e-7, a float's
+// at 1; falling with exp(-z^2 / 2) in the tail).  `density`: exp(-z^2 / 2).
+__device__ __forceinline__ float2 tail_of_normal(float2 z, float2* density) {
+    const float2 n = minus_abs(z);
+    const float2 t = reciprocal(fma2(n, pair(-0.3275911f * 0.70710678118654752f), pair(1.0f)));
+    *density = exp2_fast(mul2(mul2(z, z), pair(-0.72134752044448170f)));
+    float2 p = fma2(t, pair(0.5f * 1.061405429f), pair(0.5f * -1.453152027f));
+    p = fma2(p, t, pair(0.5f * 1.421413741f));
+    p = fma2(p, t, pair(0.5f * -0.284496736f));
+    p = fma2(p, t, pair(0.5f * 0.254829592f));
+    return mul2(mul2(p, t), *density);
+}
+
+template <int ACT> __device__ __forceinline__ float2 activate(float2 z) {
+    if (ACT == EQL_ACT_GELU) {                                // z Phi(z) = max(z, 0) - |z| Phi(-|z|)
+        float2 density;
+        const float2 q = tail_of_normal(z, &density);
+        return fma2(minus_abs(z), q, make_float2(fmaxf(z.x, 0.0f), fmaxf(z.y, 0.0f)));
+    }
+    if (ACT == EQL_ACT_SILU) return mul2(z, sigmoid(z));
     return z;
 }
-template <int ACT> __device__ __forceinline__ float slope(float z) {
-    if (ACT == EQL_ACT_GELU)
-        return 0.5f * (1.0f + erff(z * 0.70710678118654752440f)) + z * 0.39894228040143267794f * __expf(-0.5f * z * z);
-    if (ACT == EQL_ACT_SILU) {
-        const float p = __fdividef(1.0f, 1.0f + __expf(-z));
-        return p * fmaf(z, 1.0f - p, 1.0f);
+template <int ACT> __device__ __forceinline__ float2 slope(float2 z) {
+    if (ACT == EQL_ACT_GELU) {                                // Phi(z) + z phi(z)
+        float2 density;
+        const float2 h = sub2(pair(0.5f), tail_of_normal(z, &density));
+        const float2 cdf = add2(make_float2(copysignf(h.x, z.x), copysignf(h.y, z.y)), pair(0.5f));
+        return fma2(mul2(z, pair(0.39894228040143267794f)), density, cdf);
     }
-    return 1.0f;
+    if (ACT == EQL_ACT_SILU) {
+        const float2 p = sigmoid(z);
+        return mul2(p, fma2(z, sub2(pair(1.0f), p), pair(1.0f)));
+    }
+    return pair(1.0f);
 }
 
 }  // namespace eql

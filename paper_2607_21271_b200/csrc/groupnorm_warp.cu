@@ -15,9 +15,9 @@ constexpr int kThreads = 256;
 // V elements of gamma (or beta) of the columns of one vector, in x's own type.
 template <typename IO>
 __device__ __forceinline__ uint4 pack_parameter(const IO* p, float none, int element, int T) {
-    float f[NormIo<IO>::kVec];
+    float2 f[NormIo<IO>::kVec / 2];
 #pragma unroll
-    for (int j = 0; j < NormIo<IO>::kVec; ++j) f[j] = p ? NormIo<IO>::one(p, (element + j) / T) : none;
+    for (int j = 0; j < NormIo<IO>::kVec; ++j) (&f[j / 2].x)[j % 2] = p ? NormIo<IO>::one(p, (element + j) / T) : none;
     return NormIo<IO>::narrow(f);
 }
 
@@ -88,43 +88,46 @@ __global__ void __launch_bounds__(kThreads) warp_norm_kernel(NormShape s, WarpNo
         for (int k = 0; k < NV; ++k) raw[k] = next[k];
         n = b + t.step < s.B ? (int)positions_of(lengths, b + t.step, s.S) : 0;
         v.load(next, x, s, b + t.step, n);
-        float sum = 0.0f, squares = 0.0f;
+        float2 sum = pair(0.0f), squares = pair(0.0f);
 #pragma unroll
         for (int k = 0; k < NV; ++k)
             if (v.row[k] < now) {
-                float f[V];
+                float2 f[V / 2];
                 NormIo<IO>::widen(raw[k], f);
 #pragma unroll
-                for (int j = 0; j < V; ++j) sum += f[j];
+                for (int j = 0; j < V / 2; ++j) sum = add2(sum, f[j]);
             }
         const float count = (float)now * s.width;
         const float share = count > 0.0f ? __fdividef(1.0f, count) : 0.0f;
-        const float mean = lanes_sum(sum, w.lanes) * share;
+        const float mean = lanes_sum(sum.x + sum.y, w.lanes) * share;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
             if (v.row[k] < now) {
-                float f[V];
+                float2 f[V / 2];
                 NormIo<IO>::widen(raw[k], f);
 #pragma unroll
-                for (int j = 0; j < V; ++j) squares = fmaf(f[j] - mean, f[j] - mean, squares);
+                for (int j = 0; j < V / 2; ++j) {
+                    const float2 d = sub2(f[j], pair(mean));
+                    squares = fma2(d, d, squares);
+                }
             }
-        const float rstd = 1.0f / sqrtf(lanes_sum(squares, w.lanes) * share + s.eps);
+        const float rstd = 1.0f / sqrtf(lanes_sum(squares.x + squares.y, w.lanes) * share + s.eps);
         if (stats && t.active && t.lane == 0 && b < s.B) stats[b * s.groups + t.group] = make_float2(mean, rstd);
 #pragma unroll
         for (int k = 0; k < NV; ++k)
             if (v.row[k] < now) {
-                float f[V], ga[V], be[V];
+                float2 f[V / 2], ga[V / 2], be[V / 2];
                 NormIo<IO>::widen(raw[k], f);
                 NormIo<IO>::widen(gamma[k], ga);
                 NormIo<IO>::widen(beta[k], be);
 #pragma unroll
-                for (int j = 0; j < V; ++j) f[j] = activate<ACT>(fmaf((f[j] - mean) * rstd, ga[j], be[j]));
+                for (int j = 0; j < V / 2; ++j) f[j] = activate<ACT>(fma2(mul2(sub2(f[j], pair(mean)), pair(rstd)), ga[j], be[j]));
                 y[b * s.S * s.vectors + v.at[k]] = NormIo<IO>::narrow(f);
             }
     }
 }
 
-// SUMS: partial sums a vector keeps for dgamma and dbeta, 1 where its elements are of one channel, else one for each.
+// SUMS: pairs of partial sums a vector keeps for dgamma and dbeta, 1 where its elements are of one channel, else all.
 template <typename IO, int ACT, int NV, int SUMS>
 __global__ void __launch_bounds__(kThreads) warp_gradient_kernel(NormShape s, WarpNorm w, const uint4* x, const uint4* dy, const IO* gammas,
                                                                  const IO* betas, const int32_t* lengths, const float2* stats, uint4* dx, float2* parts) {
@@ -134,7 +137,7 @@ __global__ void __launch_bounds__(kThreads) warp_gradient_kernel(NormShape s, Wa
     const Seat t = seat(s, w);
     const Vectors<IO, NV> v(s, w, t);
     uint4 gamma[NV], beta[NV], rx[NV], rd[NV], nx[NV], nd[NV];
-    float db[NV][SUMS] = {}, dg[NV][SUMS] = {};
+    float2 db[NV][SUMS] = {}, dg[NV][SUMS] = {};
 #pragma unroll
     for (int k = 0; k < NV; ++k)
         if (v.row[k] != INT_MAX) {
@@ -158,46 +161,45 @@ __global__ void __launch_bounds__(kThreads) warp_gradient_kernel(NormShape s, Wa
         if (t.active && more) st = stats[(b + t.step) * s.groups + t.group];
         v.load(nx, x, s, b + t.step, n);
         v.load(nd, dy, s, b + t.step, n);
-        float s1 = 0.0f, s2 = 0.0f;
-        float xh[V], dz[V];
-        auto both = [&](int k, const float* ga) {             // xh and dz of a vector, dz not yet times gamma
-            float be[V];
+        float2 t1 = pair(0.0f), t2 = pair(0.0f), xh[V / 2], dz[V / 2];
+        auto both = [&](int k, const float2* ga) {             // xh and dz of a vector, dz not yet times gamma
+            float2 be[V / 2];
             NormIo<IO>::widen(rx[k], xh);
             NormIo<IO>::widen(rd[k], dz);
             if (ACT != EQL_ACT_NONE) NormIo<IO>::widen(beta[k], be);
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                xh[j] = (xh[j] - mean) * rstd;
-                if (ACT != EQL_ACT_NONE) dz[j] *= slope<ACT>(fmaf(xh[j], ga[j], be[j]));
+            for (int j = 0; j < V / 2; ++j) {
+                xh[j] = mul2(sub2(xh[j], pair(mean)), pair(rstd));
+                if (ACT != EQL_ACT_NONE) dz[j] = mul2(dz[j], slope<ACT>(fma2(xh[j], ga[j], be[j])));
             }
         };
 #pragma unroll
         for (int k = 0; k < NV; ++k)
             if (v.row[k] < now) {
-                float ga[V];
+                float2 ga[V / 2];
                 NormIo<IO>::widen(gamma[k], ga);
                 both(k, ga);
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    db[k][j % SUMS] += dz[j];
-                    dg[k][j % SUMS] = fmaf(dz[j], xh[j], dg[k][j % SUMS]);
-                    const float scaled = dz[j] * ga[j];
-                    s1 += scaled;
-                    s2 = fmaf(scaled, xh[j], s2);
+                for (int j = 0; j < V / 2; ++j) {
+                    db[k][j % SUMS] = add2(db[k][j % SUMS], dz[j]);
+                    dg[k][j % SUMS] = fma2(dz[j], xh[j], dg[k][j % SUMS]);
+                    const float2 scaled = mul2(dz[j], ga[j]);
+                    t1 = add2(t1, scaled);
+                    t2 = fma2(scaled, xh[j], t2);
                 }
             }
         const float count = (float)now * s.width;
         const float share = count > 0.0f ? __fdividef(1.0f, count) : 0.0f;
-        s1 = lanes_sum(s1, w.lanes) * share;
-        s2 = lanes_sum(s2, w.lanes) * share;
+        const float s1 = lanes_sum(t1.x + t1.y, w.lanes) * share, s2 = lanes_sum(t2.x + t2.y, w.lanes) * share;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
             if (v.row[k] < now) {
-                float ga[V], f[V];
+                float2 ga[V / 2], f[V / 2];
                 NormIo<IO>::widen(gamma[k], ga);
                 both(k, ga);
 #pragma unroll
-                for (int j = 0; j < V; ++j) f[j] = rstd * (fmaf(ga[j], dz[j], -s1) - xh[j] * s2);
+                for (int j = 0; j < V / 2; ++j)
+                    f[j] = mul2(pair(rstd), fma2(xh[j], pair(-s2), fma2(ga[j], dz[j], pair(-s1))));
                 dx[b * s.S * s.vectors + v.at[k]] = NormIo<IO>::narrow(f);
             }
     }
@@ -205,18 +207,25 @@ __global__ void __launch_bounds__(kThreads) warp_gradient_kernel(NormShape s, Wa
 #pragma unroll
     for (int k = 0; k < NV; ++k)
         if (t.chair < w.groups * w.instances && t.lane + w.lanes * k < w.unit) {
+            float2* to = shared + (t.chair * w.unit + t.lane + w.lanes * k) * w.sums;
 #pragma unroll
-            for (int j = 0; j < SUMS; ++j)
-                shared[(t.chair * w.unit + t.lane + w.lanes * k) * SUMS + j] = t.active ? make_float2(db[k][j], dg[k][j]) : make_float2(0.0f, 0.0f);
+            for (int j = 0; j < SUMS; ++j) {
+                if (SUMS == 1) {
+                    to[0] = make_float2(db[k][0].x + db[k][0].y, dg[k][0].x + dg[k][0].y);
+                } else {
+                    to[2 * j] = make_float2(db[k][j].x, dg[k][j].x);
+                    to[2 * j + 1] = make_float2(db[k][j].y, dg[k][j].y);
+                }
+            }
         }
     __syncthreads();
-    const int each = s.C / s.groups, runs = SUMS == 1 ? s.T / V : s.T, row = w.vectors * SUMS;
+    const int each = s.C / s.groups, runs = SUMS == 1 ? s.T / V : s.T, row = w.vectors * w.sums;
     const int block = blockIdx.x % (unsigned)w.group_blocks, cta = blockIdx.x / (unsigned)w.group_blocks;
     const int groups = min(w.groups, s.groups - block * w.groups);
     for (int c = threadIdx.x; c < groups * each; c += kThreads) {
         float2 sum = make_float2(0.0f, 0.0f);
         for (int instance = 0; instance < w.instances; ++instance) {
-            const float2* from = shared + (instance * w.groups + c / each) * w.unit * SUMS + c % each * runs;
+            const float2* from = shared + (instance * w.groups + c / each) * w.unit * w.sums + c % each * runs;
             for (int r = 0; r < (int)s.S; ++r)
                 for (int e = 0; e < runs; ++e) {
                     const float2 p = from[r * row + e];
@@ -285,8 +294,8 @@ cudaError_t launch_warp_gradient(const NormShape& s, const WarpNorm& w, eql_dtyp
             if (w.sums == 1)
                 return w.each == 1 ? launch(warp_gradient_kernel<IO, ACT, 1, 1>, limits[0]) : w.each == 2 ? launch(warp_gradient_kernel<IO, ACT, 2, 1>, limits[1])
                                    : launch(warp_gradient_kernel<IO, ACT, 4, 1>, limits[2]);
-            return w.each == 1 ? launch(warp_gradient_kernel<IO, ACT, 1, V>, limits[3]) : w.each == 2 ? launch(warp_gradient_kernel<IO, ACT, 2, V>, limits[4])
-                               : launch(warp_gradient_kernel<IO, ACT, 4, V>, limits[5]);
+            return w.each == 1 ? launch(warp_gradient_kernel<IO, ACT, 1, V / 2>, limits[3]) : w.each == 2 ? launch(warp_gradient_kernel<IO, ACT, 2, V / 2>, limits[4])
+                               : launch(warp_gradient_kernel<IO, ACT, 4, V / 2>, limits[5]);
         });
     });
 }
