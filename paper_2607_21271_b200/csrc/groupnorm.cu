@@ -3,9 +3,9 @@
 //
 // These kernels take every shape.  A CTA works on a piece of up to 256 vectors of a row, over a range of rows of one instance; a thread
 // stays with one vector column, so that what belongs to a column (statistics, gamma, sums) lies in its registers however
-// the borders of channels and groups fall.  Forward: moments of every column and row range, their merging to groups, and a pass that
-// applies them; backward: sums of dz and dz * xh of every column and row range, their merging to channels and groups, a pass that
-// applies them, and the sum over instances.  x (and dy) are read twice.
+// the borders of channels and groups fall.  Forward: moments of every range of rows, piece and group, their merging, and a pass that
+// applies them; backward: sums of dz and dz * xh of every range, piece and channel, their sums, and a pass that applies them.
+// x (and dy) are read twice; the second pass begins with the rows that the first one read last, some of which L2 still holds.
 #include <cmath>
 
 #include "groupnorm_common.cuh"
@@ -14,31 +14,36 @@ namespace eql {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kUnroll = 4;    // vectors a thread has on their way
 
 // Row ranges and pieces of an instance.
 struct Ranges {
     int pieces, ranges;       // pieces of a row, ranges of rows
     int64_t rows;             // rows of a range
-    float* columns;           // float2 [B][ranges][D], a column's partial of a range
+    int parts;                // groups (forward) or channels (backward) that a piece touches at most
+    float* partials;          // float2 [B][ranges][pieces][parts]
     float* groups;            // float2 [B][groups]: forward mean and rstd, backward the two means that dx takes off
     float* channels;          // float2 [B][C], backward
 };
 
 struct Place {
     int64_t b, row0;
-    int rows, range, vector, lane, lanes;
+    int rows, range, piece, vector, count, lane, lanes;      // count: vectors of the piece
     bool active;
+    __device__ __forceinline__ int rows_of(int l) const { return l < rows ? (rows - l + lanes - 1) / lanes : 0; }
 };
 // blockIdx.x = (b * ranges + range) * pieces + piece
-__device__ __forceinline__ Place place(const NormShape& s, const Ranges& g, const int32_t* lengths) {
+__device__ __forceinline__ Place place(const NormShape& s, const Ranges& g, const int32_t* lengths, unsigned index) {
     Place p;
-    const int64_t unit = blockIdx.x / (unsigned)g.pieces;
-    const int first = (int)(blockIdx.x % (unsigned)g.pieces) * kThreads, count = min(kThreads, s.vectors - first);
+    const int64_t unit = index / (unsigned)g.pieces;
+    p.piece = (int)(index % (unsigned)g.pieces);
+    const int first = p.piece * kThreads;
+    p.count = min(kThreads, s.vectors - first);
     p.b = unit / g.ranges;
     p.range = (int)(unit % g.ranges);
-    p.lanes = kThreads / count;
-    p.lane = threadIdx.x / count;
-    p.vector = first + threadIdx.x % count;
+    p.lanes = kThreads / p.count;
+    p.lane = threadIdx.x / p.count;
+    p.vector = first + threadIdx.x % p.count;
     p.active = p.lane < p.lanes;
     p.row0 = p.range * g.rows;
     const int64_t left = positions_of(lengths, p.b, s.S) - p.row0;
@@ -46,24 +51,46 @@ __device__ __forceinline__ Place place(const NormShape& s, const Ranges& g, cons
     return p;
 }
 
+// Part `k` (group or channel) of `each` elements, within a piece whose elements are [first, first + count): its own elements.
+struct Part {
+    int begin, end;
+    __device__ __forceinline__ Part(int k, int each, int first, int count) : begin(max(k * each, first) - first), end(min((k + 1) * each, first + count) - first) {}
+};
+
+// A column of vectors `step` apart, kUnroll of them in flight; use(i) for each.
+template <int N, typename Load, typename Use>
+__device__ __forceinline__ void walk(int count, Load&& load, Use&& use) {
+    int i = 0;
+    for (; i + kUnroll <= count; i += kUnroll) {
+        uint4 u[kUnroll][N];
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k) load(i + k, u[k]);
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k) use(i + k, u[k]);
+    }
+    for (; i < count; ++i) {
+        uint4 u[N];
+        load(i, u);
+        use(i, u);
+    }
+}
+
 template <typename IO>
-__global__ void __launch_bounds__(kThreads) column_moments_kernel(NormShape s, Ranges g, const uint4* x, const int32_t* lengths) {
+__global__ void __launch_bounds__(kThreads) part_moments_kernel(NormShape s, Ranges g, const uint4* x, const int32_t* lengths) {
     constexpr int V = NormIo<IO>::kVec;
     ptx::grid_handover();
     __shared__ float2 shared[kThreads * V];
-    const Place p = place(s, g, lengths);
+    const Place p = place(s, g, lengths, blockIdx.x);
     RunningMoments<V / 2> m;
     if (p.active) {
         const uint4* at = x + (p.b * s.S + p.row0 + p.lane) * s.vectors + p.vector;
-        for (int r = p.lane; r < p.rows; r += p.lanes, at += (int64_t)p.lanes * s.vectors) {
-            float2 f[V / 2];
-            NormIo<IO>::widen(*at, f);
-            m.add(f);
-        }
-    }
-    const int count = min(kThreads, s.vectors - (int)(blockIdx.x % (unsigned)g.pieces) * kThreads);
-    auto rows_of = [&](int lane) { return (float)((p.rows - lane + p.lanes - 1) / p.lanes); };
-    if (p.active) {
+        const int64_t step = (int64_t)p.lanes * s.vectors;
+        walk<1>(p.rows_of(p.lane), [&](int i, uint4* u) { u[0] = at[i * step]; },
+                [&](int, const uint4* u) {
+                    float2 f[V / 2];
+                    NormIo<IO>::widen(u[0], f);
+                    m.add(f);
+                });
 #pragma unroll
         for (int j = 0; j < V / 2; ++j) {
             shared[threadIdx.x * V + 2 * j] = make_float2(m.mean[j].x, m.m2[j].x);
@@ -71,32 +98,44 @@ __global__ void __launch_bounds__(kThreads) column_moments_kernel(NormShape s, R
         }
     }
     __syncthreads();
-    const int first = (int)(blockIdx.x % (unsigned)g.pieces) * kThreads * V;
-    float2* out = reinterpret_cast<float2*>(g.columns) + (p.b * g.ranges + p.range) * s.D + first;
-    for (int c = threadIdx.x; c < count * V; c += kThreads) {
+    // a column over the lanes of rows, then (its values in lane 0's place) a warp a group
+    const int first = p.piece * kThreads * V, count = p.count * V;
+    for (int c = threadIdx.x; c < count; c += kThreads) {
         Moments all{0.0f, 0.0f, 0.0f};
         for (int l = 0; l < p.lanes && l < p.rows; ++l) {
-            const float2 v = shared[l * count * V + c];
-            all = merge(all, Moments{rows_of(l), v.x, v.y});
+            const float2 v = shared[l * count + c];
+            all = merge(all, Moments{(float)p.rows_of(l), v.x, v.y});
         }
-        out[c] = make_float2(all.mean, all.m2);
+        shared[c] = make_float2(all.mean, all.m2);
+    }
+    __syncthreads();
+    const int group0 = first / s.width, groups = (first + count - 1) / s.width - group0 + 1;
+    float2* out = reinterpret_cast<float2*>(g.partials) + ((p.b * g.ranges + p.range) * g.pieces + p.piece) * g.parts;
+    for (int k = threadIdx.x >> 5; k < groups; k += kThreads / 32) {
+        const Part part(group0 + k, s.width, first, count);
+        Moments all{0.0f, 0.0f, 0.0f};
+        for (int c = part.begin + (threadIdx.x & 31); c < part.end; c += 32) all = merge(all, Moments{(float)p.rows, shared[c].x, shared[c].y});
+        all = warp_merge(all);
+        if ((threadIdx.x & 31) == 0) out[k] = make_float2(all.mean, all.m2);
     }
 }
 
 // One CTA an instance and group.
-__global__ void __launch_bounds__(kThreads) group_moments_kernel(NormShape s, Ranges g, const int32_t* lengths, float* stats) {
+__global__ void __launch_bounds__(kThreads) group_moments_kernel(NormShape s, Ranges g, int V, const int32_t* lengths, float* stats) {
     ptx::grid_handover();
     __shared__ Moments shared[kThreads / 32];
     const int64_t b = blockIdx.x / (unsigned)s.groups;
-    const int group = (int)(blockIdx.x % (unsigned)s.groups);
+    const int group = (int)(blockIdx.x % (unsigned)s.groups), size = kThreads * V;
     const int64_t n = positions_of(lengths, b, s.S);
-    const float2* columns = reinterpret_cast<const float2*>(g.columns) + b * g.ranges * s.D + group * s.width;
+    const int piece0 = group * s.width / size, pieces = ((group + 1) * s.width - 1) / size - piece0 + 1;
     Moments all{0.0f, 0.0f, 0.0f};
-    for (int64_t i = threadIdx.x; i < (int64_t)g.ranges * s.width; i += kThreads) {
-        const int64_t range = i / s.width, left = n - range * g.rows;
+    for (int i = threadIdx.x; i < g.ranges * pieces; i += kThreads) {
+        const int range = i / pieces, piece = piece0 + i % pieces;
+        const int64_t left = n - range * g.rows;
+        const Part part(group, s.width, piece * size, min(size, s.D - piece * size));
         const float rows = (float)(left < 0 ? 0 : left < g.rows ? left : g.rows);
-        const float2 v = columns[range * s.D + i % s.width];
-        all = merge(all, Moments{rows, v.x, v.y});
+        const float2 v = reinterpret_cast<const float2*>(g.partials)[((b * g.ranges + range) * g.pieces + piece) * g.parts + group - piece * size / s.width];
+        all = merge(all, Moments{rows * (part.end - part.begin), v.x, v.y});
     }
     all = warp_merge(all);
     if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = all;
@@ -132,45 +171,46 @@ __global__ void __launch_bounds__(kThreads) apply_kernel(NormShape s, Ranges g, 
                                                          const int32_t* lengths, uint4* y) {
     constexpr int V = NormIo<IO>::kVec;
     ptx::grid_handover();
-    const Place p = place(s, g, lengths);
+    const Place p = place(s, g, lengths, gridDim.x - 1 - blockIdx.x);
     if (!p.active || p.lane >= p.rows) return;
     Column<IO> c(s, reinterpret_cast<const float2*>(g.groups), gamma, beta, p.b, p.vector);
 #pragma unroll
     for (int j = 0; j < V / 2; ++j) c.gamma[j] = mul2(c.gamma[j], c.rstd[j]);
-    int64_t at = (p.b * s.S + p.row0 + p.lane) * s.vectors + p.vector;
-    for (int r = p.lane; r < p.rows; r += p.lanes, at += (int64_t)p.lanes * s.vectors) {
-        float2 f[V / 2];
-        NormIo<IO>::widen(x[at], f);
+    const int64_t at = (p.b * s.S + p.row0 + p.lane) * s.vectors + p.vector, step = (int64_t)p.lanes * s.vectors;
+    walk<1>(p.rows_of(p.lane), [&](int i, uint4* u) { u[0] = x[at + i * step]; },
+            [&](int i, const uint4* u) {
+                float2 f[V / 2];
+                NormIo<IO>::widen(u[0], f);
 #pragma unroll
-        for (int j = 0; j < V / 2; ++j) f[j] = activate<ACT>(fma2(sub2(f[j], c.mean[j]), c.gamma[j], c.beta[j]));
-        y[at] = NormIo<IO>::narrow(f);
-    }
+                for (int j = 0; j < V / 2; ++j) f[j] = activate<ACT>(fma2(sub2(f[j], c.mean[j]), c.gamma[j], c.beta[j]));
+                y[at + i * step] = NormIo<IO>::narrow(f);
+            });
 }
 
 template <typename IO, int ACT>
-__global__ void __launch_bounds__(kThreads) column_sums_kernel(NormShape s, Ranges g, const uint4* x, const uint4* dy, const IO* gamma, const IO* beta,
-                                                               const int32_t* lengths, const float* stats) {
+__global__ void __launch_bounds__(kThreads) part_sums_kernel(NormShape s, Ranges g, const uint4* x, const uint4* dy, const IO* gamma, const IO* beta,
+                                                             const int32_t* lengths, const float* stats) {
     constexpr int V = NormIo<IO>::kVec;
     ptx::grid_handover();
     __shared__ float2 shared[kThreads * V];
-    const Place p = place(s, g, lengths);
+    const Place p = place(s, g, lengths, blockIdx.x);
     float2 db[V / 2] = {}, dg[V / 2] = {};
     if (p.active && p.lane < p.rows) {
         const Column<IO> c(s, reinterpret_cast<const float2*>(stats), gamma, beta, p.b, p.vector);
-        int64_t at = (p.b * s.S + p.row0 + p.lane) * s.vectors + p.vector;
-        for (int r = p.lane; r < p.rows; r += p.lanes, at += (int64_t)p.lanes * s.vectors) {
-            float2 f[V / 2], d[V / 2];
-            NormIo<IO>::widen(x[at], f);
-            NormIo<IO>::widen(dy[at], d);
+        const int64_t at = (p.b * s.S + p.row0 + p.lane) * s.vectors + p.vector, step = (int64_t)p.lanes * s.vectors;
+        walk<2>(p.rows_of(p.lane), [&](int i, uint4* u) { u[0] = x[at + i * step]; u[1] = dy[at + i * step]; },
+                [&](int, const uint4* u) {
+                    float2 f[V / 2], d[V / 2];
+                    NormIo<IO>::widen(u[0], f);
+                    NormIo<IO>::widen(u[1], d);
 #pragma unroll
-            for (int j = 0; j < V / 2; ++j) {
-                const float2 xh = mul2(sub2(f[j], c.mean[j]), c.rstd[j]), dz = mul2(d[j], slope<ACT>(fma2(xh, c.gamma[j], c.beta[j])));
-                db[j] = add2(db[j], dz);
-                dg[j] = fma2(dz, xh, dg[j]);
-            }
-        }
+                    for (int j = 0; j < V / 2; ++j) {
+                        const float2 xh = mul2(sub2(f[j], c.mean[j]), c.rstd[j]), dz = mul2(d[j], slope<ACT>(fma2(xh, c.gamma[j], c.beta[j])));
+                        db[j] = add2(db[j], dz);
+                        dg[j] = fma2(dz, xh, dg[j]);
+                    }
+                });
     }
-    const int first = (int)(blockIdx.x % (unsigned)g.pieces) * kThreads, count = min(kThreads, s.vectors - first);
     if (p.active) {
 #pragma unroll
         for (int j = 0; j < V / 2; ++j) {
@@ -179,14 +219,38 @@ __global__ void __launch_bounds__(kThreads) column_sums_kernel(NormShape s, Rang
         }
     }
     __syncthreads();
-    float2* out = reinterpret_cast<float2*>(g.columns) + (p.b * g.ranges + p.range) * s.D + first * V;
-    for (int c = threadIdx.x; c < count * V; c += kThreads) {
+    const int first = p.piece * kThreads * V, count = p.count * V;
+    const int channel0 = first / s.T, channels = (first + count - 1) / s.T - channel0 + 1;
+    float2* out = reinterpret_cast<float2*>(g.partials) + ((p.b * g.ranges + p.range) * g.pieces + p.piece) * g.parts;
+    for (int k = threadIdx.x; k < channels; k += kThreads) {
+        const Part part(channel0 + k, s.T, first, count);
         float2 all = make_float2(0.0f, 0.0f);
-        for (int l = 0; l < p.lanes; ++l) {
-            const float2 v = shared[l * count * V + c];
-            all.x += v.x; all.y += v.y;
+        for (int l = 0; l < p.lanes && l < p.rows; ++l)
+            for (int c = part.begin; c < part.end; ++c) all = add2(all, shared[l * count + c]);
+        out[k] = all;
+    }
+}
+
+// A channel of an instance over all ranges (and the two pieces that a channel can lie in): eight channels a CTA and 32 chains.
+__global__ void __launch_bounds__(kThreads) channel_sums_kernel(NormShape s, Ranges g, int V) {
+    ptx::grid_handover();
+    __shared__ float2 shared[kThreads];
+    const int blocks = (s.C + 7) / 8, size = kThreads * V;
+    const int64_t b = blockIdx.x / (unsigned)blocks;
+    const int channel = (int)(blockIdx.x % (unsigned)blocks) * 8 + (threadIdx.x & 7);
+    float2 sum = make_float2(0.0f, 0.0f);
+    if (channel < s.C) {
+        const int piece0 = channel * s.T / size, pieces = ((channel + 1) * s.T - 1) / size - piece0 + 1;
+        for (int i = threadIdx.x >> 3; i < g.ranges * pieces; i += kThreads / 8) {
+            const int range = i / pieces, piece = piece0 + i % pieces;
+            sum = add2(sum, reinterpret_cast<const float2*>(g.partials)[((b * g.ranges + range) * g.pieces + piece) * g.parts + channel - piece * size / s.T]);
         }
-        out[c] = all;
+    }
+    shared[threadIdx.x] = sum;
+    __syncthreads();
+    if (threadIdx.x < 8 && channel < s.C) {
+        for (int k = 1; k < kThreads / 8; ++k) sum = add2(sum, shared[k * 8 + threadIdx.x]);
+        reinterpret_cast<float2*>(g.channels)[b * s.C + channel] = sum;
     }
 }
 
@@ -199,34 +263,24 @@ __device__ __forceinline__ float2 warp_sum(float2 v) {
     return v;
 }
 
-// One CTA an instance and group: a warp adds up a channel, whose tuple and row ranges its lanes share.
+// One warp an instance and group.
 template <typename IO>
 __global__ void __launch_bounds__(kThreads) group_sums_kernel(NormShape s, Ranges g, const IO* gamma, const int32_t* lengths) {
     ptx::grid_handover();
-    __shared__ float2 shared[kThreads / 32];
-    const int64_t b = blockIdx.x / (unsigned)s.groups;
-    const int group = (int)(blockIdx.x % (unsigned)s.groups), each = s.C / s.groups, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t unit = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+    if (unit >= s.B * s.groups) return;
+    const int64_t b = unit / s.groups;
+    const int group = (int)(unit % s.groups), each = s.C / s.groups;
     float2 total = make_float2(0.0f, 0.0f);
-    for (int k = warp; k < each; k += kThreads / 32) {
+    for (int k = threadIdx.x & 31; k < each; k += 32) {
         const int channel = group * each + k;
-        const float2* columns = reinterpret_cast<const float2*>(g.columns) + b * g.ranges * s.D + (int64_t)channel * s.T;
-        float2 sum = make_float2(0.0f, 0.0f);
-        for (int64_t i = lane; i < (int64_t)g.ranges * s.T; i += 32) {
-            const float2 v = columns[i / s.T * s.D + i % s.T];
-            sum.x += v.x; sum.y += v.y;
-        }
-        sum = warp_sum(sum);
-        if (lane == 0) reinterpret_cast<float2*>(g.channels)[b * s.C + channel] = sum;
         const float w = gamma ? NormIo<IO>::one(gamma, channel) : 1.0f;
-        total.x = fmaf(w, sum.x, total.x);
-        total.y = fmaf(w, sum.y, total.y);
+        total = fma2(pair(w), reinterpret_cast<const float2*>(g.channels)[b * s.C + channel], total);
     }
-    if (lane == 0) shared[warp] = total;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < kThreads / 32; ++w) { total.x += shared[w].x; total.y += shared[w].y; }
+    total = warp_sum(total);
+    if ((threadIdx.x & 31) == 0) {
         const float n = (float)positions_of(lengths, b, s.S) * s.width;
-        reinterpret_cast<float2*>(g.groups)[blockIdx.x] = n > 0.0f ? make_float2(total.x / n, total.y / n) : make_float2(0.0f, 0.0f);
+        reinterpret_cast<float2*>(g.groups)[unit] = n > 0.0f ? make_float2(total.x / n, total.y / n) : make_float2(0.0f, 0.0f);
     }
 }
 
@@ -235,7 +289,7 @@ __global__ void __launch_bounds__(kThreads) apply_gradient_kernel(NormShape s, R
                                                                   const int32_t* lengths, const float* stats, uint4* dx) {
     constexpr int V = NormIo<IO>::kVec;
     ptx::grid_handover();
-    const Place p = place(s, g, lengths);
+    const Place p = place(s, g, lengths, gridDim.x - 1 - blockIdx.x);
     if (!p.active || p.lane >= p.rows) return;
     const Column<IO> c(s, reinterpret_cast<const float2*>(stats), gamma, beta, p.b, p.vector);
     float2 off1[V / 2], off2[V / 2];
@@ -245,18 +299,19 @@ __global__ void __launch_bounds__(kThreads) apply_gradient_kernel(NormShape s, R
         (&off1[j / 2].x)[j % 2] = -v.x;
         (&off2[j / 2].x)[j % 2] = -v.y;
     }
-    int64_t at = (p.b * s.S + p.row0 + p.lane) * s.vectors + p.vector;
-    for (int r = p.lane; r < p.rows; r += p.lanes, at += (int64_t)p.lanes * s.vectors) {
-        float2 f[V / 2], d[V / 2];
-        NormIo<IO>::widen(x[at], f);
-        NormIo<IO>::widen(dy[at], d);
+    const int64_t at = (p.b * s.S + p.row0 + p.lane) * s.vectors + p.vector, step = (int64_t)p.lanes * s.vectors;
+    walk<2>(p.rows_of(p.lane), [&](int i, uint4* u) { u[0] = x[at + i * step]; u[1] = dy[at + i * step]; },
+            [&](int i, const uint4* u) {
+                float2 f[V / 2], d[V / 2];
+                NormIo<IO>::widen(u[0], f);
+                NormIo<IO>::widen(u[1], d);
 #pragma unroll
-        for (int j = 0; j < V / 2; ++j) {
-            const float2 xh = mul2(sub2(f[j], c.mean[j]), c.rstd[j]), dz = mul2(d[j], slope<ACT>(fma2(xh, c.gamma[j], c.beta[j])));
-            f[j] = mul2(c.rstd[j], fma2(xh, off2[j], fma2(c.gamma[j], dz, off1[j])));
-        }
-        dx[at] = NormIo<IO>::narrow(f);
-    }
+                for (int j = 0; j < V / 2; ++j) {
+                    const float2 xh = mul2(sub2(f[j], c.mean[j]), c.rstd[j]), dz = mul2(d[j], slope<ACT>(fma2(xh, c.gamma[j], c.beta[j])));
+                    f[j] = mul2(c.rstd[j], fma2(xh, off2[j], fma2(c.gamma[j], dz, off1[j])));
+                }
+                dx[at + i * step] = NormIo<IO>::narrow(f);
+            });
 }
 
 // dgamma and dbeta: the sum over `parts` rows of float2 [parts][C], eight channels a CTA and 32 chains.
@@ -295,19 +350,22 @@ eql_status_t check_norm(const eql_groupnorm_t* n, NormShape* s) {
     return EQL_OK;
 }
 
-// Ranges of rows so that a launch fills the device a few times over, of 64 rows at least (the partials are then a small share of the data).
-Ranges range_plan(const NormShape& s, char* scratch, size_t* bytes) {
+// Ranges of rows so that a launch fills the device a few times over, of 32 rows at least.
+Ranges range_plan(const NormShape& s, eql_dtype_t dtype, bool backward, char* scratch, size_t* bytes) {
     Ranges g{};
+    const int V = dtype == EQL_FP32 ? 4 : 8;
     g.pieces = (s.vectors + kThreads - 1) / kThreads;
     const int64_t wanted = (8 * kNumSMs + s.B * g.pieces - 1) / (s.B * g.pieces);
-    const int64_t most = s.S / 64 > 1 ? s.S / 64 : 1;
+    const int64_t most = s.S / 32 > 1 ? s.S / 32 : 1;
     const int64_t ranges = wanted < most ? wanted : most;
     g.rows = (s.S + ranges - 1) / ranges;
     g.ranges = (int)((s.S + g.rows - 1) / g.rows);
+    const int elements = s.D < kThreads * V ? s.D : kThreads * V, each = backward ? s.T : s.width;
+    g.parts = (elements + each - 2) / each + 1;
     size_t off = 0;
-    g.columns = (float*)(scratch + off);   off += align_up((size_t)s.B * g.ranges * s.D * 8, kWsAlign);
+    g.partials = (float*)(scratch + off);  off += align_up((size_t)s.B * g.ranges * g.pieces * g.parts * 8, kWsAlign);
     g.groups = (float*)(scratch + off);    off += align_up((size_t)s.B * s.groups * 8, kWsAlign);
-    g.channels = (float*)(scratch + off);  off += align_up((size_t)s.B * s.C * 8, kWsAlign);
+    g.channels = (float*)(scratch + off);  if (backward) off += align_up((size_t)s.B * s.C * 8, kWsAlign);
     *bytes = off;
     return g;
 }
@@ -333,8 +391,8 @@ NormPlan norm_plan(const NormShape& s, eql_dtype_t dtype, bool backward, char* s
         p.scratch_bytes = backward ? align_up((size_t)s.B * p.resident.cluster * s.C * 8, kWsAlign) : 0;
         return p;
     }
-    p.ranges = range_plan(s, scratch, &p.scratch_bytes);
-    p.fits = s.B * p.ranges.ranges * p.ranges.pieces <= INT32_MAX && s.B * s.groups <= INT32_MAX;
+    p.ranges = range_plan(s, dtype, backward, scratch, &p.scratch_bytes);
+    p.fits = s.B * p.ranges.ranges * p.ranges.pieces <= INT32_MAX && s.B * s.groups <= INT32_MAX && s.B * ((s.C + 7) / 8) <= INT32_MAX;
     return p;
 }
 
@@ -348,8 +406,8 @@ cudaError_t run_ranges(const NormShape& s, const Ranges& g, eql_dtype_t dtype, c
     const int64_t grid = s.B * g.ranges * g.pieces, units = s.B * s.groups;
     return dispatch_io(dtype, [&](auto io) {
         using IO = decltype(io);
-        cudaError_t err = launch_overlapped(column_moments_kernel<IO>, dim3((unsigned)grid), dim3(kThreads), 0, st, s, g, (const uint4*)x, lengths);
-        if (err == cudaSuccess) err = launch_overlapped(group_moments_kernel, dim3((unsigned)units), dim3(kThreads), 0, st, s, g, lengths, stats);
+        cudaError_t err = launch_overlapped(part_moments_kernel<IO>, dim3((unsigned)grid), dim3(kThreads), 0, st, s, g, (const uint4*)x, lengths);
+        if (err == cudaSuccess) err = launch_overlapped(group_moments_kernel, dim3((unsigned)units), dim3(kThreads), 0, st, s, g, NormIo<IO>::kVec, lengths, stats);
         if (err != cudaSuccess) return err;
         return dispatch_act(s.act, [&](auto act) {
             return launch_overlapped(apply_kernel<IO, decltype(act)::value>, dim3((unsigned)grid), dim3(kThreads), 0, st, s, g, (const uint4*)x,
@@ -365,10 +423,13 @@ cudaError_t run_ranges_gradient(const NormShape& s, const Ranges& g, eql_dtype_t
         using IO = decltype(io);
         return dispatch_act(s.act, [&](auto act) {
             constexpr int ACT = decltype(act)::value;
-            cudaError_t err = launch_overlapped(column_sums_kernel<IO, ACT>, dim3((unsigned)grid), dim3(kThreads), 0, st, s, g, (const uint4*)x,
+            cudaError_t err = launch_overlapped(part_sums_kernel<IO, ACT>, dim3((unsigned)grid), dim3(kThreads), 0, st, s, g, (const uint4*)x,
                                                 (const uint4*)dy, (const IO*)gamma, (const IO*)beta, lengths, stats);
             if (err == cudaSuccess)
-                err = launch_overlapped(group_sums_kernel<IO>, dim3((unsigned)units), dim3(kThreads), 0, st, s, g, (const IO*)gamma, lengths);
+                err = launch_overlapped(channel_sums_kernel, dim3((unsigned)(s.B * ((s.C + 7) / 8))), dim3(kThreads), 0, st, s, g, NormIo<IO>::kVec);
+            if (err == cudaSuccess)
+                err = launch_overlapped(group_sums_kernel<IO>, dim3((unsigned)((units + kThreads / 32 - 1) / (kThreads / 32))), dim3(kThreads), 0, st, s, g,
+                                        (const IO*)gamma, lengths);
             if (err == cudaSuccess)
                 err = launch_overlapped(apply_gradient_kernel<IO, ACT>, dim3((unsigned)grid), dim3(kThreads), 0, st, s, g, (const uint4*)x,
                                         (const uint4*)dy, (const IO*)gamma, (const IO*)beta, lengths, stats, (uint4*)dx);

@@ -281,6 +281,7 @@ SHAPES = [
     (16, 64, 1, 37, 1), (2, 4, 1, 5, 1), (1, 8, 1, 3, 1), (32, 33, 11, 2, 5), (12, 10, 5, 1, 130), (1, 4096, 1, 2, 3), (6, 4, 2, 1, 3000),
     (8, 96, 1, 130, 1), (2, 8, 8, 300, 2), (64, 2, 2, 4, 31), (1, 16, 16, 2, 1100), (7, 40, 8, 3, 64), (4, 24, 1, 1, 5000),
     (1, 1000, 8, 2, 70), (8, 1100, 2, 2, 9), (1, 2056, 257, 3, 4),
+    (12, 700, 2, 2, 40), (3, 2736, 1, 2, 70), (4, 24, 8, 1, 20000), (1, 16, 16, 1, 40001),
 ]
 
 
