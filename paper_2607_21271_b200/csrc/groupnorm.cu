@@ -388,7 +388,7 @@ NormPlan norm_plan(const NormShape& s, eql_dtype_t dtype, bool backward, char* s
     }
     p.resident = resident_norm_plan(s, dtype, backward);
     if (p.resident.supported) {
-        p.scratch_bytes = backward ? align_up((size_t)s.B * p.resident.cluster * s.C * 8, kWsAlign) : 0;
+        p.scratch_bytes = backward ? align_up((size_t)p.resident.instances * p.resident.cluster * s.C * 8, kWsAlign) : 0;
         return p;
     }
     p.ranges = range_plan(s, dtype, backward, scratch, &p.scratch_bytes);
@@ -521,7 +521,7 @@ eql_status_t eqlinear_groupnorm_bwd(const eql_groupnorm_t* norm, const void* x, 
     } else if (p.resident.supported) {
         e = launch_resident_gradient(s, p.resident, dtype, x, dy, gamma, beta, lengths, stats, dx, (float*)scratch, st);
         if (e == cudaSuccess)
-            e = launch_parameter_sums((const float*)scratch, s.B * p.resident.cluster, s.C, (float*)dgamma, (float*)dbeta, st);
+            e = launch_parameter_sums((const float*)scratch, (int64_t)p.resident.instances * p.resident.cluster, s.C, (float*)dgamma, (float*)dbeta, st);
     } else {
         e = run_ranges_gradient(s, p.ranges, dtype, x, dy, gamma, beta, lengths, stats, dx, (float*)dgamma, (float*)dbeta, st);
     }

@@ -46,6 +46,7 @@ struct ResidentNorm {
     bool supported;
     int groups, blocks;       // groups of a block, blocks of a row
     int cluster, threads;     // CTAs of a unit, threads of a CTA
+    int instances;            // instances that are worked on side by side
     int64_t rows;             // rows of a CTA
     int run, sums, share;     // backward: neighbouring elements summed up in a thread, sums of a vector, lanes that add up a channel
     int slot_bytes, side_offset, shared_bytes;
@@ -54,7 +55,7 @@ constexpr int kResidentShared = 220 * 1024;
 ResidentNorm resident_norm_plan(const NormShape& s, eql_dtype_t dtype, bool backward);
 cudaError_t launch_resident_norm(const NormShape& s, const ResidentNorm& r, eql_dtype_t dtype, const void* x, const void* gamma, const void* beta,
                                  const int32_t* lengths, void* y, float* stats, cudaStream_t stream);
-// parts: float2 [B * cluster][C], the CTAs' sums of dz and dz * xh
+// parts: float2 [instances * cluster][C], the CTAs' sums of dz and dz * xh
 cudaError_t launch_resident_gradient(const NormShape& s, const ResidentNorm& r, eql_dtype_t dtype, const void* x, const void* dy, const void* gamma,
                                      const void* beta, const int32_t* lengths, const float* stats, void* dx, float* parts, cudaStream_t stream);
 

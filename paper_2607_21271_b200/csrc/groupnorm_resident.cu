@@ -3,8 +3,8 @@
 // A unit is a block of whole groups of one instance, at least 128 bytes of every row where there are as many.  It belongs to one CTA, or to a
 // cluster whose CTAs hold a range of its rows each; what they have to tell each other is one triple (forward) or pair (backward) a
 // group, written into every CTA's shared memory.  A thread stays with one 16-byte column, which it copies asynchronously into slots of its own: no
-// barrier stands between copy and use, and as many bytes are in flight as shared memory holds.
-// What bounds it is the memory; several CTAs to an SM overlap one's reading with another's writing.
+// barrier stands between copy and use, as many bytes are in flight as shared memory holds, and a slot that has been read for the last
+// time takes a vector of the next instance at once.  What belongs to a column stays in registers for all instances that a CTA takes.
 #include "groupnorm_common.cuh"
 
 namespace eql {
@@ -23,61 +23,88 @@ __device__ __forceinline__ void store_remote(uint32_t address, float a, float b,
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(address + 8), "f"(c) : "memory");
 }
 
-// Where a thread stands: its unit, its rows and its column.
+// Where a thread stands: its block of groups, its column, its lane of rows, and its first instance.
 struct Post {
-    int64_t b;
-    int first_group, groups;  // of the unit
-    int vector, column, columns;      // vector of the row; the same within the unit, of how many
+    int64_t b, row0;
+    int first_group, groups;  // of the block
+    int vector, column, columns;      // vector of the row; the same within the block, of how many
     int lane, lanes, rank;
-    int rows, each, extra;    // rows of this CTA: so many for each lane, and one more for the first few
-    int64_t row0;
     bool active;
-    __device__ __forceinline__ int rows_of(int l) const { return each + (l < extra ? 1 : 0); }
+    __device__ __forceinline__ Post(const NormShape& s, const ResidentNorm& r, int V) {
+        const unsigned unit = blockIdx.x / (unsigned)r.cluster, block = unit % (unsigned)r.blocks;
+        rank = blockIdx.x % (unsigned)r.cluster;
+        b = unit / (unsigned)r.blocks;
+        first_group = block * r.groups;
+        groups = min(r.groups, s.groups - first_group);
+        columns = groups * s.width / V;
+        lanes = blockDim.x / (unsigned)columns;
+        lane = threadIdx.x / (unsigned)columns;
+        column = threadIdx.x - lane * columns;
+        vector = first_group * s.width / V + column;
+        active = lane < lanes;
+        row0 = (int64_t)rank * r.rows;
+    }
+    // this thread's first vector of an instance
+    __device__ __forceinline__ int64_t at(const NormShape& s, int64_t instance) const { return (instance * s.S + row0 + lane) * s.vectors + vector; }
 };
-__device__ __forceinline__ Post post(const NormShape& s, const ResidentNorm& r, const int32_t* lengths, int V) {
-    Post p;
-    p.rank = blockIdx.x % (unsigned)r.cluster;
-    const int64_t unit = blockIdx.x / (unsigned)r.cluster;
-    p.b = unit / r.blocks;
-    const int block = (int)(unit % r.blocks);
-    p.first_group = block * r.groups;
-    p.groups = min(r.groups, s.groups - p.first_group);
-    p.columns = p.groups * s.width / V;
-    p.lanes = blockDim.x / (unsigned)p.columns;
-    p.lane = threadIdx.x / (unsigned)p.columns;
-    p.column = threadIdx.x % (unsigned)p.columns;
-    p.vector = p.first_group * s.width / V + p.column;
-    p.active = p.lane < p.lanes;
-    p.row0 = (int64_t)p.rank * r.rows;
-    const int64_t left = positions_of(lengths, p.b, s.S) - p.row0;
-    p.rows = (int)(left < 0 ? 0 : left < r.rows ? left : r.rows);
-    p.each = p.rows / p.lanes;
-    p.extra = p.rows % p.lanes;
-    return p;
-}
+// The rows that a CTA has of an instance, dealt to its lanes: so many each, one more for the first few.
+struct Rows {
+    int all, each, extra;
+    __device__ __forceinline__ Rows(const NormShape& s, const ResidentNorm& r, const Post& p, const int32_t* lengths, int64_t b) {
+        const int64_t left = b < s.B ? positions_of(lengths, b, s.S) - p.row0 : 0;
+        all = (int)(left < 0 ? 0 : left < r.rows ? left : r.rows);
+        each = all / (unsigned)p.lanes;
+        extra = all - each * p.lanes;
+    }
+    __device__ __forceinline__ int of(int lane) const { return each + (lane < extra ? 1 : 0); }
+};
+// e / d for e below 2^16 and d up to 2^16, by a reciprocal computed once: ceil(2^32 / d).
+struct Divisor {
+    unsigned d, inverse;
+    __device__ __forceinline__ explicit Divisor(unsigned by) : d(by), inverse(by > 1 ? 0xffffffffu / by + 1 : 0) {}
+    __device__ __forceinline__ unsigned operator()(unsigned e) const { return d > 1 ? __umulhi(e, inverse) : e; }
+};
 
-// Shared memory, behind the slots: results a group (float2), what the cluster's CTAs sent ([CTA][group] of three floats), and the room
-// in which threads put their partial results side by side.
+// Shared memory, behind the slots: results a group (float2), what the cluster's CTAs sent (for this instance and the one before:
+// [2][CTA][group] of three floats), and the room in which threads put their partial results side by side.
 struct Room {
     uint4* slots;
     float2* result;
     float* sent;
     float2* side;
+    __device__ __forceinline__ Room(const ResidentNorm& r, uint8_t* shared) {
+        slots = reinterpret_cast<uint4*>(shared);
+        result = reinterpret_cast<float2*>(shared + r.slot_bytes);
+        sent = reinterpret_cast<float*>(result + r.groups);
+        side = reinterpret_cast<float2*>(shared + r.side_offset);
+    }
+    __device__ __forceinline__ float* from(const ResidentNorm& r, int round, int rank, int group) const {
+        return sent + (((round & 1) * r.cluster + rank) * r.groups + group) * 3;
+    }
+    // A warp has this CTA's values of a group: its lanes write them into every CTA of the cluster.  (Into the half that the other
+    // CTAs read an instance ago: they have all passed the barrier of the one in between.)
+    __device__ __forceinline__ void send(const ResidentNorm& r, int round, int rank, int group, float a, float b, float c) const {
+        const int lane = threadIdx.x & 31;
+        if (lane < r.cluster) store_remote(ptx::map_to_cta(ptx::smem_u32(from(r, round, rank, group)), lane), a, b, c);
+    }
 };
-__device__ __forceinline__ Room room(const ResidentNorm& r, uint8_t* shared) {
-    Room m;
-    m.slots = reinterpret_cast<uint4*>(shared);
-    m.result = reinterpret_cast<float2*>(shared + r.slot_bytes);
-    m.sent = reinterpret_cast<float*>(m.result + r.groups);
-    m.side = reinterpret_cast<float2*>(shared + r.side_offset);
-    return m;
-}
 
-// A warp has this CTA's values of a group: its lanes write them into every CTA of the cluster.
-__device__ __forceinline__ void send(const Room& m, const ResidentNorm& r, int rank, int group, float a, float b, float c) {
-    const int lane = threadIdx.x & 31;
-    if (lane < r.cluster) store_remote(ptx::map_to_cta(ptx::smem_u32(m.sent + (rank * r.groups + group) * 3), lane), a, b, c);
-}
+// Copies of an instance's vectors into the thread's slots, in two groups: the first half can be used while the second is on its way.
+// They are issued one by one, when a slot has been read for the last time.
+struct Fetch {
+    int count, half;
+    __device__ __forceinline__ explicit Fetch(int n) : count(n), half((n + 1) / 2) {}
+    template <typename Copy>
+    __device__ __forceinline__ void operator()(int i, Copy&& copy) const {
+        if (i >= count) return;
+        if (i == half) copies_commit();
+        copy(i);
+    }
+    __device__ __forceinline__ void end() const {
+        if (count <= half) copies_commit();
+        copies_commit();
+    }
+};
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
@@ -108,256 +135,342 @@ __device__ __forceinline__ Moments moments_of(int entries, At&& at) {
     return Moments{count, mean, warp_sum(m2)};
 }
 
-template <typename IO, int ACT, int THREADS>
-__global__ void __launch_bounds__(THREADS) resident_norm_kernel(NormShape s, ResidentNorm r, const uint4* x, const IO* gammas, const IO* betas,
-                                                                const int32_t* lengths, uint4* y, float2* stats) {
+// What belongs to the elements of a vector: N = 1 where they are of one channel (and so of one group), else a pair for each two.
+// value(channel, group) for every element; the divisions by T and by a group's width are done once.
+template <int N, int V, typename Set>
+__device__ __forceinline__ void each_element(const NormShape& s, int vector, Set&& set) {
+    int channel = vector * V / s.T, in_channel = vector * V - channel * s.T, group = vector * V / s.width, in_group = vector * V - group * s.width;
+#pragma unroll
+    for (int j = 0; j < (N == 1 ? 1 : V); ++j) {
+        set(j, channel, group);
+        if (++in_channel == s.T) { in_channel = 0; ++channel; }
+        if (++in_group == s.width) { in_group = 0; ++group; }
+    }
+}
+template <int N> __device__ __forceinline__ float2 of_pair(const float2 (&v)[N], int j) { return N == 1 ? v[0] : v[j]; }
+template <int N> __device__ __forceinline__ void put(float2 (&v)[N], int j, float value) {
+    if (N == 1) v[0] = pair(value);
+    else (&v[j / 2].x)[j % 2] = value;
+}
+
+// N: see each_element.
+template <typename IO, int ACT, int N, int THREADS, int CTAS>
+__global__ void __launch_bounds__(THREADS, CTAS) resident_norm_kernel(NormShape s, ResidentNorm r, const uint4* x, const IO* gammas, const IO* betas,
+                                                                      const int32_t* lengths, uint4* y, float2* stats) {
     constexpr int V = NormIo<IO>::kVec, P = V / 2;
     extern __shared__ __align__(128) uint8_t shared[];
-    const Room m = room(r, shared);
+    const Room m(r, shared);
     ptx::grid_handover();
     __syncwarp();
     if (r.cluster > 1) ptx::cluster_arrive();
-    const Post p = post(s, r, lengths, V);
-    const int mine = p.active ? p.rows_of(p.lane) : 0, half = (mine + 1) / 2, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    const uint4* from = x + (p.b * s.S + p.row0 + p.lane) * s.vectors + p.vector;
+    const Post p(s, r, V);
+    const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5, pitch = blockDim.x;
     const int64_t step = (int64_t)p.lanes * s.vectors;
     uint4* slot = m.slots + threadIdx.x;
-    const int pitch = blockDim.x;
-    for (int i = 0; i < half; ++i, from += step) copy_async16(slot + i * pitch, from);
-    copies_commit();
-    for (int i = half; i < mine; ++i, from += step) copy_async16(slot + i * pitch, from);
-    copies_commit();
-
-    RunningMoments<P> moments;
-    auto add = [&](int i) {
-        float2 f[P];
-        NormIo<IO>::widen(slot[i * pitch], f);
-        moments.add(f);
-    };
-    copies_wait<1>();
-    for (int i = 0; i < half; ++i) add(i);
-    copies_wait<0>();
-    for (int i = half; i < mine; ++i) add(i);
-
-    const bool whole = s.width % V == 0;                      // a vector lies in one group
-    if (whole) {                                              // the columns of a vector have as many values each
-        float mean = 0.0f, m2 = 0.0f;
-#pragma unroll
-        for (int j = 0; j < V; ++j) mean += element(moments.mean, j);
-        mean *= 1.0f / V;
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const float d = element(moments.mean, j) - mean;
-            m2 += fmaf(moments.rows * d, d, element(moments.m2, j));
-        }
-        if (p.groups == 1) {                                  // every thread's: a warp's together
-            const Moments t = moments_of(32, [&](int, float* n) { *n = moments.rows * V; return make_float2(mean, m2); });
-            if ((threadIdx.x & 31) == 0) { m.side[2 * warp] = make_float2(t.mean, t.m2); m.side[2 * warp + 1].x = t.n; }
-        } else {
-            m.side[threadIdx.x] = make_float2(mean, m2);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j) m.side[threadIdx.x * V + j] = make_float2(element(moments.mean, j), element(moments.m2, j));
+    Rows rows(s, r, p, lengths, p.b);
+    int mine = p.active ? rows.of(p.lane) : 0;
+    {
+        const Fetch fetch(mine);
+        const uint4* from = x + p.at(s, p.b);
+        for (int i = 0; i < mine; ++i, from += step) fetch(i, [&](int k) { copy_async16(slot + k * pitch, from); });
+        fetch.end();
     }
-    __syncthreads();
-    if (r.cluster > 1) ptx::cluster_wait();                   // the other CTAs have started: their shared memory may be written
-    for (int g = warp; g < p.groups; g += warps) {
-        Moments t;
-        if (whole && p.groups == 1) {
-            t = moments_of(warps, [&](int e, float* n) { *n = m.side[2 * e + 1].x; return m.side[2 * e]; });
-        } else {
-            // entries of a lane of rows: the group's vectors, or where they cross its border its elements
-            const int per = whole ? 1 : V, width = whole ? s.width / V : s.width, pitch_of = p.columns * per;
-            t = moments_of(min(p.lanes, p.rows) * width, [&](int e, float* n) {
-                const int l = e / (unsigned)width;
-                *n = (float)(p.rows_of(l) * (V / per));
-                return m.side[l * pitch_of + g * width + e - l * width];
-            });
-        }
-        if (r.cluster > 1) {
-            send(m, r, p.rank, g, t.n, t.mean, t.m2);
-        } else if ((threadIdx.x & 31) == 0) {
-            const float2 out = make_float2(t.mean, rstd_of(t, s.eps));
-            m.result[g] = out;
-            if (stats) stats[p.b * s.groups + p.first_group + g] = out;
-        }
-    }
-    __syncthreads();
-    if (r.cluster > 1) {
-        ptx::cluster_arrive();
-        ptx::cluster_wait();
-        for (int g = threadIdx.x; g < p.groups; g += blockDim.x) {
-            Moments t{0.0f, 0.0f, 0.0f};
-            for (int c = 0; c < r.cluster; ++c) {
-                const float* at = m.sent + (c * r.groups + g) * 3;
-                t = merge(t, Moments{at[0], at[1], at[2]});
+    float2 gamma[N], beta[N];
+    each_element<N, V>(s, p.vector, [&](int j, int channel, int) {
+        put(gamma, j, p.active && gammas ? NormIo<IO>::one(gammas, channel) : 1.0f);
+        put(beta, j, p.active && betas ? NormIo<IO>::one(betas, channel) : 0.0f);
+    });
+    const bool whole = N == 1 || s.width % V == 0;            // a vector lies in one group
+    const Divisor width(whole ? s.width / V : s.width);
+    int round = 0;
+    for (int64_t b = p.b; b < s.B; b += r.instances, ++round) {
+        RunningMoments<P> moments;
+        auto add = [&](int i) {
+            float2 f[P];
+            NormIo<IO>::widen(slot[i * pitch], f);
+            moments.add(f);
+        };
+        const int half = (mine + 1) / 2;
+        copies_wait<1>();
+        for (int i = 0; i < half; ++i) add(i);
+        copies_wait<0>();
+        for (int i = half; i < mine; ++i) add(i);
+        if (whole) {                                          // the columns of a vector have as many values each
+            float mean = 0.0f, m2 = 0.0f;
+#pragma unroll
+            for (int j = 0; j < V; ++j) mean += element(moments.mean, j);
+            mean *= 1.0f / V;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float d = element(moments.mean, j) - mean;
+                m2 += fmaf(moments.rows * d, d, element(moments.m2, j));
             }
-            const float2 out = make_float2(t.mean, rstd_of(t, s.eps));
-            m.result[g] = out;
-            if (stats && p.rank == 0) stats[p.b * s.groups + p.first_group + g] = out;
+            if (p.groups == 1) {                              // every thread's: a warp's together
+                const Moments t = moments_of(32, [&](int, float* n) { *n = moments.rows * V; return make_float2(mean, m2); });
+                if ((threadIdx.x & 31) == 0) { m.side[2 * warp] = make_float2(t.mean, t.m2); m.side[2 * warp + 1].x = t.n; }
+            } else {
+                m.side[threadIdx.x] = make_float2(mean, m2);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) m.side[threadIdx.x * V + j] = make_float2(element(moments.mean, j), element(moments.m2, j));
         }
         __syncthreads();
-    }
-    if (mine == 0) return;
-    float2 mean[P], scale[P], beta[P];
+        if (r.cluster > 1 && round == 0) ptx::cluster_wait(); // the other CTAs have started: their shared memory may be written
+        for (int g = warp; g < p.groups; g += warps) {
+            Moments t;
+            if (whole && p.groups == 1) {
+                t = moments_of(warps, [&](int e, float* n) { *n = m.side[2 * e + 1].x; return m.side[2 * e]; });
+            } else {
+                // entries of a lane of rows: the group's vectors, or where they cross its border its elements
+                const int per = whole ? 1 : V, row = p.columns * per;
+                t = moments_of(min(p.lanes, rows.all) * (int)width.d, [&](int e, float* n) {
+                    const int l = width(e);
+                    *n = (float)(rows.of(l) * (V / per));
+                    return m.side[l * row + (g - l) * (int)width.d + e];
+                });
+            }
+            if (r.cluster > 1) {
+                m.send(r, round, p.rank, g, t.n, t.mean, t.m2);
+            } else if ((threadIdx.x & 31) == 0) {
+                const float2 out = make_float2(t.mean, rstd_of(t, s.eps));
+                m.result[g] = out;
+                if (stats) stats[b * s.groups + p.first_group + g] = out;
+            }
+        }
+        __syncthreads();
+        if (r.cluster > 1) {
+            ptx::cluster_arrive();
+            ptx::cluster_wait();
+            for (int g = threadIdx.x; g < p.groups; g += blockDim.x) {
+                Moments t{0.0f, 0.0f, 0.0f};
+                for (int c = 0; c < r.cluster; ++c) {
+                    const float* at = m.from(r, round, c, g);
+                    t = merge(t, Moments{at[0], at[1], at[2]});
+                }
+                const float2 out = make_float2(t.mean, rstd_of(t, s.eps));
+                m.result[g] = out;
+                if (stats && p.rank == 0) stats[b * s.groups + p.first_group + g] = out;
+            }
+            __syncthreads();
+        }
+        float2 mean[N], scale[N];
+        each_element<N, V>(s, p.vector, [&](int j, int, int group) {
+            const float2 v = m.result[p.active ? group - p.first_group : 0];
+            put(mean, j, v.x);
+            put(scale, j, v.y);
+        });
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const int channel = (p.vector * V + j) / s.T;
-        const float2 v = m.result[(p.column * V + j) / s.width];
-        (&mean[j / 2].x)[j % 2] = v.x;
-        (&scale[j / 2].x)[j % 2] = gammas ? NormIo<IO>::one(gammas, channel) * v.y : v.y;
-        (&beta[j / 2].x)[j % 2] = betas ? NormIo<IO>::one(betas, channel) : 0.0f;
-    }
-    uint4* to = y + (p.b * s.S + p.row0 + p.lane) * s.vectors + p.vector;
-    for (int i = 0; i < mine; ++i, to += step) {
-        float2 f[P];
-        NormIo<IO>::widen(slot[i * pitch], f);
+        for (int j = 0; j < N; ++j) scale[j] = mul2(scale[j], gamma[j]);
+        // every slot, once used, takes the next instance's vector
+        const Rows next(s, r, p, lengths, b + r.instances);
+        const Fetch fetch(p.active ? next.of(p.lane) : 0);
+        uint4* to = y + p.at(s, b);
+        const uint4* from = x + p.at(s, b + r.instances);
+        auto refill = [&](int i) { fetch(i, [&](int k) { copy_async16(slot + k * pitch, from); }); from += step; };
+        for (int i = 0; i < mine; ++i, to += step) {
+            float2 f[P];
+            NormIo<IO>::widen(slot[i * pitch], f);
 #pragma unroll
-        for (int j = 0; j < P; ++j) f[j] = activate<ACT>(fma2(sub2(f[j], mean[j]), scale[j], beta[j]));
-        *to = NormIo<IO>::narrow(f);
+            for (int j = 0; j < P; ++j) f[j] = activate<ACT>(fma2(sub2(f[j], of_pair(mean, j)), of_pair(scale, j), of_pair(beta, j)));
+            *to = NormIo<IO>::narrow(f);
+            refill(i);
+        }
+        for (int i = mine; i < fetch.count; ++i) refill(i);
+        fetch.end();
+        rows = next;
+        mine = fetch.count;
     }
 }
 
-template <typename IO, int ACT, int THREADS>
-__global__ void __launch_bounds__(THREADS) resident_gradient_kernel(NormShape s, ResidentNorm r, const uint4* x, const uint4* dy, const IO* gammas,
-                                                                    const IO* betas, const int32_t* lengths, const float2* stats, uint4* dx, float2* parts) {
+template <typename IO, int ACT, int N, int THREADS, int CTAS>
+__global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormShape s, ResidentNorm r, const uint4* x, const uint4* dy, const IO* gammas,
+                                                                          const IO* betas, const int32_t* lengths, const float2* stats, uint4* dx,
+                                                                          float2* parts) {
     constexpr int V = NormIo<IO>::kVec, P = V / 2;
     extern __shared__ __align__(128) uint8_t shared[];
-    const Room m = room(r, shared);
+    const Room m(r, shared);
     ptx::grid_handover();
     __syncwarp();
     if (r.cluster > 1) ptx::cluster_arrive();
-    const Post p = post(s, r, lengths, V);
-    const int mine = p.active ? p.rows_of(p.lane) : 0, half = (mine + 1) / 2, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t start = (p.b * s.S + p.row0 + p.lane) * s.vectors + p.vector, step = (int64_t)p.lanes * s.vectors;
+    const Post p(s, r, V);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t step = (int64_t)p.lanes * s.vectors;
     uint4* slot = m.slots + threadIdx.x;
     const int pitch = 2 * blockDim.x, second = blockDim.x;    // x and dy of a row are neighbours
-    int64_t at = start;
-    auto fetch = [&](int i) {
-        copy_async16(slot + i * pitch, x + at);
-        copy_async16(slot + i * pitch + second, dy + at);
-        at += step;
-    };
-    for (int i = 0; i < half; ++i) fetch(i);
-    copies_commit();
-    for (int i = half; i < mine; ++i) fetch(i);
-    copies_commit();
-    float2 gamma[P], beta[P], mean[P], rstd[P];
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const int element = p.vector * V + j, channel = element / s.T;
-        const float2 v = p.active ? stats[p.b * s.groups + element / s.width] : make_float2(0.0f, 0.0f);
-        (&gamma[j / 2].x)[j % 2] = p.active && gammas ? NormIo<IO>::one(gammas, channel) : 1.0f;
-        (&beta[j / 2].x)[j % 2] = p.active && betas ? NormIo<IO>::one(betas, channel) : 0.0f;
-        (&mean[j / 2].x)[j % 2] = v.x;
-        (&rstd[j / 2].x)[j % 2] = v.y;
+    Rows rows(s, r, p, lengths, p.b);
+    int mine = p.active ? rows.of(p.lane) : 0;
+    {
+        const Fetch fetch(mine);
+        int64_t at = p.at(s, p.b);
+        for (int i = 0; i < mine; ++i, at += step)
+            fetch(i, [&](int k) { copy_async16(slot + k * pitch, x + at); copy_async16(slot + k * pitch + second, dy + at); });
+        fetch.end();
     }
-    float2 db[P] = {}, dg[P] = {}, xh[P], dz[P];
-    auto both = [&](int i) {
-        NormIo<IO>::widen(slot[i * pitch], xh);
-        NormIo<IO>::widen(slot[i * pitch + second], dz);
+    float2 gamma[N], beta[N];
+    each_element<N, V>(s, p.vector, [&](int j, int channel, int) {
+        put(gamma, j, p.active && gammas ? NormIo<IO>::one(gammas, channel) : 1.0f);
+        put(beta, j, p.active && betas ? NormIo<IO>::one(betas, channel) : 0.0f);
+    });
+    const int each = s.C / s.groups, channels = p.groups * each, row = p.columns * r.sums;
+    const Divisor runs(s.T / r.run);
+    float2* sums = m.side + blockDim.x * r.sums;              // a channel's, of this instance and of all so far
+    float2* total = sums + r.groups * each;
+    const int teams = blockDim.x / (unsigned)r.share, team = threadIdx.x / (unsigned)r.share;
+    for (int c = threadIdx.x; c < channels; c += blockDim.x) total[c] = make_float2(0.0f, 0.0f);
+    int round = 0;
+    for (int64_t b = p.b; b < s.B; b += r.instances, ++round) {
+        // z = (x - mean) * (rstd * gamma) + beta;  rstd comes to the sums of dz * (x - mean) at the end
+        float2 mean[N], scale[N], rstd[N];
+        each_element<N, V>(s, p.vector, [&](int j, int, int group) {
+            const float2 v = p.active ? stats[b * s.groups + group] : make_float2(0.0f, 0.0f);
+            put(mean, j, v.x);
+            put(rstd, j, v.y);
+        });
 #pragma unroll
-        for (int j = 0; j < P; ++j) {
-            xh[j] = mul2(sub2(xh[j], mean[j]), rstd[j]);
-            if (ACT != EQL_ACT_NONE) dz[j] = mul2(dz[j], slope<ACT>(fma2(xh[j], gamma[j], beta[j])));
-        }
-    };
-    auto add = [&](int i) {
-        both(i);
+        for (int j = 0; j < N; ++j) scale[j] = mul2(rstd[j], gamma[j]);
+        float2 db[P] = {}, dg[P] = {}, xc[P], dz[P];
+        auto both = [&](int i) {
+            NormIo<IO>::widen(slot[i * pitch], xc);
+            NormIo<IO>::widen(slot[i * pitch + second], dz);
 #pragma unroll
-        for (int j = 0; j < P; ++j) {
-            db[j] = add2(db[j], dz[j]);
-            dg[j] = fma2(dz[j], xh[j], dg[j]);
-        }
-    };
-    copies_wait<1>();
-    for (int i = 0; i < half; ++i) add(i);
-    copies_wait<0>();
-    for (int i = half; i < mine; ++i) add(i);
+            for (int j = 0; j < P; ++j) {
+                xc[j] = sub2(xc[j], of_pair(mean, j));
+                if (ACT != EQL_ACT_NONE) dz[j] = mul2(dz[j], slope<ACT>(fma2(xc[j], of_pair(scale, j), of_pair(beta, j))));
+            }
+        };
+        auto add = [&](int i) {
+            both(i);
+#pragma unroll
+            for (int j = 0; j < P; ++j) {
+                const int k = N == 1 ? j % 2 : j;             // (two chains are enough where one number comes out)
+                db[k] = add2(db[k], dz[j]);
+                dg[k] = fma2(dz[j], xc[j], dg[k]);
+            }
+        };
+        const int half = (mine + 1) / 2;
+        copies_wait<1>();
+        for (int i = 0; i < half; ++i) add(i);
+        copies_wait<0>();
+        for (int i = half; i < mine; ++i) add(i);
 
-    // The thread's sums side by side: r.sums of them, of r.run neighbouring elements each (a channel's).
-    float2 run = make_float2(0.0f, 0.0f);
+        // The thread's sums side by side: r.sums of them, of r.run neighbouring elements each (a channel's).
+        if (N == 1) {
+            db[0] = add2(db[0], db[1]);
+            dg[0] = mul2(add2(dg[0], dg[1]), rstd[0]);
+            m.side[threadIdx.x] = make_float2(db[0].x + db[0].y, dg[0].x + dg[0].y);
+        } else {
+            float2 run = make_float2(0.0f, 0.0f);
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        run.x += element(db, j);
-        run.y += element(dg, j);
-        if ((j + 1) % r.run == 0) {
-            m.side[threadIdx.x * r.sums + j / r.run] = run;
-            run = make_float2(0.0f, 0.0f);
-        }
-    }
-    __syncthreads();
-    // Channels: `share` lanes each, over the lanes of rows and the runs of the tuple.
-    const int each = s.C / s.groups, channels = p.groups * each, runs = s.T / r.run, row = p.columns * r.sums;
-    float2* sums = m.side + blockDim.x * r.sums;              // a channel's
-    const int teams = blockDim.x / (unsigned)r.share, entries = min(p.lanes, p.rows) * runs, team = threadIdx.x / (unsigned)r.share;
-    for (int c0 = 0; c0 < channels; c0 += teams) {
-        const int c = c0 + team;
-        float2 v = make_float2(0.0f, 0.0f);
-        if (c < channels)
-            for (int e = threadIdx.x - team * r.share; e < entries; e += r.share) {
-                const int l = e / (unsigned)runs;
-                v = add2(v, m.side[l * row + c * runs + e - l * runs]);
+            for (int j = 0; j < P; ++j) dg[j] = mul2(dg[j], of_pair(rstd, j));
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                run.x += element(db, j);
+                run.y += element(dg, j);
+                if ((j + 1) % r.run == 0) {
+                    m.side[threadIdx.x * r.sums + j / r.run] = run;
+                    run = make_float2(0.0f, 0.0f);
+                }
             }
-        for (int d = r.share >> 1; d > 0; d >>= 1) {
-            v.x += __shfl_xor_sync(0xffffffffu, v.x, d);
-            v.y += __shfl_xor_sync(0xffffffffu, v.y, d);
-        }
-        if (c < channels && threadIdx.x == team * r.share) {
-            sums[c] = v;
-            parts[(p.b * r.cluster + p.rank) * s.C + p.first_group * each + c] = v;
-        }
-    }
-    __syncthreads();
-    if (r.cluster > 1) ptx::cluster_wait();
-    const float count = (float)positions_of(lengths, p.b, s.S) * s.width, share = count > 0.0f ? 1.0f / count : 0.0f;
-    for (int g = warp; g < p.groups; g += blockDim.x >> 5) {
-        float2 v = make_float2(0.0f, 0.0f);
-        for (int c = lane; c < each; c += 32) {
-            const float w = gammas ? NormIo<IO>::one(gammas, (p.first_group + g) * each + c) : 1.0f;
-            v = fma2(pair(w), sums[g * each + c], v);
-        }
-        v.x = warp_sum(v.x);
-        v.y = warp_sum(v.y);
-        if (r.cluster > 1) send(m, r, p.rank, g, v.x, v.y, 0.0f);
-        else if (lane == 0) m.result[g] = make_float2(v.x * share, v.y * share);
-    }
-    __syncthreads();
-    if (r.cluster > 1) {
-        ptx::cluster_arrive();
-        ptx::cluster_wait();
-        for (int g = threadIdx.x; g < p.groups; g += blockDim.x) {
-            float2 v = make_float2(0.0f, 0.0f);
-            for (int c = 0; c < r.cluster; ++c) {
-                const float* from = m.sent + (c * r.groups + g) * 3;
-                v.x += from[0]; v.y += from[1];
-            }
-            m.result[g] = make_float2(v.x * share, v.y * share);
         }
         __syncthreads();
-    }
-    if (mine == 0) return;
-    float2 off1[P], off2[P];
+        // Channels: `share` lanes each, over the lanes of rows and the runs of the tuple.
+        const int entries = min(p.lanes, rows.all) * (int)runs.d;
+        for (int c0 = 0; c0 < channels; c0 += teams) {
+            const int c = c0 + team;
+            float2 v = make_float2(0.0f, 0.0f);
+            if (c < channels)
+                for (int e = threadIdx.x - team * r.share; e < entries; e += r.share) {
+                    const int l = runs(e);
+                    v = add2(v, m.side[l * row + (c - l) * (int)runs.d + e]);
+                }
+            for (int d = r.share >> 1; d > 0; d >>= 1) {
+                v.x += __shfl_xor_sync(0xffffffffu, v.x, d);
+                v.y += __shfl_xor_sync(0xffffffffu, v.y, d);
+            }
+            if (c < channels && threadIdx.x == team * r.share) {
+                sums[c] = v;
+                total[c] = add2(total[c], v);
+            }
+        }
+        __syncthreads();
+        if (r.cluster > 1 && round == 0) ptx::cluster_wait();
+        const float count = (float)positions_of(lengths, b, s.S) * s.width, share = count > 0.0f ? 1.0f / count : 0.0f;
+        for (int g = warp; g < p.groups; g += blockDim.x >> 5) {
+            float2 v = make_float2(0.0f, 0.0f);
+            for (int c = lane; c < each; c += 32) {
+                const float w = gammas ? NormIo<IO>::one(gammas, (p.first_group + g) * each + c) : 1.0f;
+                v = fma2(pair(w), sums[g * each + c], v);
+            }
+            v.x = warp_sum(v.x);
+            v.y = warp_sum(v.y);
+            if (r.cluster > 1) m.send(r, round, p.rank, g, v.x, v.y, 0.0f);
+            else if (lane == 0) m.result[g] = make_float2(v.x * share, v.y * share);
+        }
+        __syncthreads();
+        if (r.cluster > 1) {
+            ptx::cluster_arrive();
+            ptx::cluster_wait();
+            for (int g = threadIdx.x; g < p.groups; g += blockDim.x) {
+                float2 v = make_float2(0.0f, 0.0f);
+                for (int c = 0; c < r.cluster; ++c) {
+                    const float* from = m.from(r, round, c, g);
+                    v.x += from[0]; v.y += from[1];
+                }
+                m.result[g] = make_float2(v.x * share, v.y * share);
+            }
+            __syncthreads();
+        }
+        // dx = dz * (rstd * gamma) - (x - mean) * (rstd * rstd * second) - rstd * first
+        float2 off1[N], off2[N];
+        each_element<N, V>(s, p.vector, [&](int j, int, int group) {
+            const float2 v = m.result[p.active ? group - p.first_group : 0];
+            put(off1, j, -v.x);
+            put(off2, j, -v.y);
+        });
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const float2 v = m.result[(p.column * V + j) / s.width];
-        (&off1[j / 2].x)[j % 2] = -v.x;
-        (&off2[j / 2].x)[j % 2] = -v.y;
-    }
-    uint4* to = dx + start;
-    for (int i = 0; i < mine; ++i, to += step) {
-        both(i);
-        float2 f[P];
+        for (int j = 0; j < N; ++j) {
+            off1[j] = mul2(off1[j], rstd[j]);
+            off2[j] = mul2(mul2(off2[j], rstd[j]), rstd[j]);
+        }
+        const Rows next(s, r, p, lengths, b + r.instances);
+        const Fetch fetch(p.active ? next.of(p.lane) : 0);
+        uint4* to = dx + p.at(s, b);
+        int64_t at = p.at(s, b + r.instances);
+        auto refill = [&](int i) {
+            fetch(i, [&](int k) { copy_async16(slot + k * pitch, x + at); copy_async16(slot + k * pitch + second, dy + at); });
+            at += step;
+        };
+        for (int i = 0; i < mine; ++i, to += step) {
+            both(i);
+            float2 f[P];
 #pragma unroll
-        for (int j = 0; j < P; ++j) f[j] = mul2(rstd[j], fma2(xh[j], off2[j], fma2(gamma[j], dz[j], off1[j])));
-        *to = NormIo<IO>::narrow(f);
+            for (int j = 0; j < P; ++j) f[j] = fma2(xc[j], of_pair(off2, j), fma2(dz[j], of_pair(scale, j), of_pair(off1, j)));
+            *to = NormIo<IO>::narrow(f);
+            refill(i);
+        }
+        for (int i = mine; i < fetch.count; ++i) refill(i);
+        fetch.end();
+        rows = next;
+        mine = fetch.count;
     }
+    float2* out = parts + (p.b * r.cluster + p.rank) * s.C + p.first_group * each;
+    for (int c0 = 0; c0 < channels; c0 += teams)               // (each by the thread that added it up)
+        if (c0 + team < channels && threadIdx.x == team * r.share) out[c0 + team] = total[c0 + team];
 }
 
 }  // namespace
 
 constexpr int kFewThreads = 256, kManyForward = 1024, kManyBackward = 512;
+#ifndef TUNE_FWD_CTAS
+#define TUNE_FWD_CTAS 4
+#define TUNE_BWD_CTAS1 3
+#define TUNE_BWD_CTAS 2
+#define TUNE_SHARED 74
+#define TUNE_PERSIST 1
+#endif
+// CTAs of 256 threads to an SM, by the registers that the kernels then may use.
+constexpr int kForwardCtas = TUNE_FWD_CTAS, kGradientCtasTuple = TUNE_BWD_CTAS1, kGradientCtas = TUNE_BWD_CTAS;
 
 ResidentNorm resident_norm_plan(const NormShape& s, eql_dtype_t dtype, bool backward) {
     ResidentNorm r{};
@@ -378,11 +491,11 @@ ResidentNorm resident_norm_plan(const NormShape& s, eql_dtype_t dtype, bool back
     r.run = s.T % V == 0 ? V : V % s.T == 0 ? s.T : 1;
     r.sums = V / r.run;
     const int channels = r.groups * (s.C / s.groups), lanes = (int)(r.threads / columns);
-    const int side = backward ? r.threads * r.sums + channels : s.width % V == 0 ? r.threads : r.threads * V;
+    const int side = backward ? r.threads * r.sums + 2 * channels : s.width % V == 0 ? r.threads : r.threads * V;
     for (r.cluster = 1; r.cluster <= kMaxCluster; r.cluster *= 2) {
         r.rows = (s.S + r.cluster - 1) / r.cluster;
         const int64_t slots = (r.rows + lanes - 1) / lanes, slot_bytes = slots * r.threads * 16 * (backward ? 2 : 1);
-        r.side_offset = (int)align_up((size_t)r.groups * 8 + (size_t)r.cluster * r.groups * 12, 16);
+        r.side_offset = (int)align_up((size_t)r.groups * 8 + (size_t)r.cluster * r.groups * 24, 16);
         const int64_t all = slot_bytes + r.side_offset + side * 8;
         if (all <= kResidentShared) {
             r.slot_bytes = (int)slot_bytes;
@@ -390,13 +503,26 @@ ResidentNorm resident_norm_plan(const NormShape& s, eql_dtype_t dtype, bool back
             r.shared_bytes = (int)all;
             r.supported = true;
             // larger clusters until three CTAs fit an SM, and every SM has one or a thread has no more than four vectors
-            if (all <= 74 * 1024 && (s.B * r.blocks * r.cluster >= kNumSMs || slots <= 4)) break;
+            if (all <= TUNE_SHARED * 1024 && (s.B * r.blocks * r.cluster >= kNumSMs || slots <= 4)) break;
         }
         if (r.cluster == kMaxCluster) break;
     }
+    if (!r.supported) return r;
     r.share = 1;
     while (r.share < 32 && r.share * 2 * channels <= r.threads) r.share *= 2;
-    r.supported = r.supported && s.B * r.blocks * r.cluster <= INT32_MAX;
+    // One CTA after the other takes a block's instances, as many side by side as are resident together, and all about the same number.
+    // (A cluster takes one: how many of them are resident depends on the SMs that the device has in each of its parts.)
+    int64_t together = 228 * 1024 / (r.shared_bytes + 1024), most = backward ? (s.T % V == 0 ? kGradientCtasTuple : kGradientCtas) : kForwardCtas;
+    if (r.threads != kFewThreads) most = 1;
+    if (together > most) together = most;
+    together = together * kNumSMs / (r.blocks * r.cluster);
+    if (together < 1) together = 1;
+    r.instances = (int)s.B;
+    if (TUNE_PERSIST && r.cluster == 1 && together < s.B) {
+        const int64_t rounds = (s.B + together - 1) / together;
+        r.instances = (int)((s.B + rounds - 1) / rounds);
+    }
+    r.supported = (int64_t)r.instances * r.blocks * r.cluster <= INT32_MAX;
     return r;
 }
 
@@ -409,7 +535,7 @@ static cudaError_t launch_resident(Kernel kernel, SmemLimitOnce& limit, const No
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
     attr[1].val.clusterDim.x = (unsigned)r.cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
-    cfg.gridDim = dim3((unsigned)(s.B * r.blocks * r.cluster));
+    cfg.gridDim = dim3((unsigned)((int64_t)r.instances * r.blocks * r.cluster));
     cfg.blockDim = dim3(r.threads); cfg.dynamicSmemBytes = r.shared_bytes; cfg.stream = stream;
     cfg.attrs = attr; cfg.numAttrs = r.cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, s, r, args...);
@@ -419,12 +545,16 @@ cudaError_t launch_resident_norm(const NormShape& s, const ResidentNorm& r, eql_
                                  const int32_t* lengths, void* y, float* stats, cudaStream_t stream) {
     return dispatch_io(dtype, [&](auto io) {
         using IO = decltype(io);
+        constexpr int V = NormIo<IO>::kVec, P = V / 2;
         return dispatch_act(s.act, [&](auto act) {
             constexpr int ACT = decltype(act)::value;
-            static SmemLimitOnce limits[2];
-            const bool few = r.threads == kFewThreads;
-            return launch_resident(few ? resident_norm_kernel<IO, ACT, kFewThreads> : resident_norm_kernel<IO, ACT, kManyForward>, limits[few], s, r, stream, (const uint4*)x, (const IO*)gamma, (const IO*)beta,
-                                   lengths, (uint4*)y, (float2*)stats);
+            static SmemLimitOnce limits[3];
+            auto launch = [&](auto kernel, SmemLimitOnce& limit) {
+                return launch_resident(kernel, limit, s, r, stream, (const uint4*)x, (const IO*)gamma, (const IO*)beta, lengths, (uint4*)y, (float2*)stats);
+            };
+            if (r.threads != kFewThreads) return launch(resident_norm_kernel<IO, ACT, P, kManyForward, 1>, limits[0]);
+            return s.T % V == 0 ? launch(resident_norm_kernel<IO, ACT, 1, kFewThreads, kForwardCtas>, limits[1])
+                                : launch(resident_norm_kernel<IO, ACT, P, kFewThreads, kForwardCtas>, limits[2]);
         });
     });
 }
@@ -433,12 +563,17 @@ cudaError_t launch_resident_gradient(const NormShape& s, const ResidentNorm& r, 
                                      const void* beta, const int32_t* lengths, const float* stats, void* dx, float* parts, cudaStream_t stream) {
     return dispatch_io(dtype, [&](auto io) {
         using IO = decltype(io);
+        constexpr int V = NormIo<IO>::kVec, P = V / 2;
         return dispatch_act(s.act, [&](auto act) {
             constexpr int ACT = decltype(act)::value;
-            static SmemLimitOnce limits[2];
-            const bool few = r.threads == kFewThreads;
-            return launch_resident(few ? resident_gradient_kernel<IO, ACT, kFewThreads> : resident_gradient_kernel<IO, ACT, kManyBackward>, limits[few], s, r, stream, (const uint4*)x, (const uint4*)dy,
-                                   (const IO*)gamma, (const IO*)beta, lengths, (const float2*)stats, (uint4*)dx, (float2*)parts);
+            static SmemLimitOnce limits[3];
+            auto launch = [&](auto kernel, SmemLimitOnce& limit) {
+                return launch_resident(kernel, limit, s, r, stream, (const uint4*)x, (const uint4*)dy, (const IO*)gamma, (const IO*)beta, lengths,
+                                       (const float2*)stats, (uint4*)dx, (float2*)parts);
+            };
+            if (r.threads != kFewThreads) return launch(resident_gradient_kernel<IO, ACT, P, kManyBackward, 1>, limits[0]);
+            return s.T % V == 0 ? launch(resident_gradient_kernel<IO, ACT, 1, kFewThreads, kGradientCtasTuple>, limits[1])
+                                : launch(resident_gradient_kernel<IO, ACT, P, kFewThreads, kGradientCtas>, limits[2]);
         });
     });
 }
