@@ -161,6 +161,17 @@ __device__ __forceinline__ Moments warp_merge(Moments v) {
     }
     return v;                 // lane 0's
 }
+__device__ __forceinline__ float exp2_fast(float v) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float reciprocal(float v) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+
 // The running form (Welford 1962) for columns of 2 P values, row after row: a fourth operation an element, and unlike with sums behind a
 // fixed pivot it does not matter how far the first value lies from the rest.
 template <int P>
@@ -169,7 +180,7 @@ struct RunningMoments {
     float2 mean[P] = {}, m2[P] = {};
     __device__ __forceinline__ void add(const float2* f) {
         rows += 1.0f;
-        const float2 share = pair(__fdividef(1.0f, rows));
+        const float2 share = pair(reciprocal(rows));
 #pragma unroll
         for (int j = 0; j < P; ++j) {
             const float2 d = sub2(f[j], mean[j]);
@@ -186,16 +197,6 @@ __device__ __forceinline__ int64_t positions_of(const int32_t* lengths, int64_t 
     return n < 0 ? 0 : n > S ? S : n;
 }
 
-__device__ __forceinline__ float exp2_fast(float v) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-    return r;
-}
-__device__ __forceinline__ float reciprocal(float v) {
-    float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-    return r;
-}
 __device__ __forceinline__ float2 exp2_fast(float2 v) { return make_float2(exp2_fast(v.x), exp2_fast(v.y)); }
 __device__ __forceinline__ float2 reciprocal(float2 v) { return make_float2(reciprocal(v.x), reciprocal(v.y)); }
 

@@ -89,22 +89,24 @@ struct Room {
     }
 };
 
-// Copies of an instance's vectors into the thread's slots, in two groups: the first half can be used while the second is on its way.
-// They are issued one by one, when a slot has been read for the last time.
-struct Fetch {
-    int count, half;
-    __device__ __forceinline__ explicit Fetch(int n) : count(n), half((n + 1) / 2) {}
-    template <typename Copy>
-    __device__ __forceinline__ void operator()(int i, Copy&& copy) const {
-        if (i >= count) return;
-        if (i == half) copies_commit();
+// use(i) for the `mine` slots of one instance, and copy(i) into the `count` slots of the next one, each slot as soon as it has been used;
+// the copies in two groups, so that the first half can be used while the second is on its way.
+template <typename Use, typename Copy>
+__device__ __forceinline__ void refill(int mine, int count, Use&& use, Copy&& copy) {
+    const int half = (count + 1) / 2;
+    int i = 0;
+    for (; i < half; ++i) {
+        if (i < mine) use(i);
         copy(i);
     }
-    __device__ __forceinline__ void end() const {
-        if (count <= half) copies_commit();
-        copies_commit();
+    copies_commit();
+    for (; i < count; ++i) {
+        if (i < mine) use(i);
+        copy(i);
     }
-};
+    copies_commit();
+    for (; i < mine; ++i) use(i);
+}
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
@@ -135,17 +137,35 @@ __device__ __forceinline__ Moments moments_of(int entries, At&& at) {
     return Moments{count, mean, warp_sum(m2)};
 }
 
+// The groups of a vector's elements, relative to its first element's: three bits each.
+template <int N, int V>
+__device__ __forceinline__ unsigned group_steps(const NormShape& s, int vector) {
+    unsigned steps = 0;
+    if (N > 1) {
+        int in_group = vector * V % s.width, step = 0;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            steps |= step << (3 * j);
+            if (++in_group == s.width) { in_group = 0; ++step; }
+        }
+    }
+    return steps;
+}
 // What belongs to the elements of a vector: N = 1 where they are of one channel (and so of one group), else a pair for each two.
-// value(channel, group) for every element; the divisions by T and by a group's width are done once.
+// set(element, channel) for every element, and set(element, group) with the steps above.
 template <int N, int V, typename Set>
-__device__ __forceinline__ void each_element(const NormShape& s, int vector, Set&& set) {
-    int channel = vector * V / s.T, in_channel = vector * V - channel * s.T, group = vector * V / s.width, in_group = vector * V - group * s.width;
+__device__ __forceinline__ void each_channel(const NormShape& s, int vector, Set&& set) {
+    int channel = vector * V / s.T, in_channel = vector * V - channel * s.T;
 #pragma unroll
     for (int j = 0; j < (N == 1 ? 1 : V); ++j) {
-        set(j, channel, group);
+        set(j, channel);
         if (++in_channel == s.T) { in_channel = 0; ++channel; }
-        if (++in_group == s.width) { in_group = 0; ++group; }
     }
+}
+template <int N, int V, typename Set>
+__device__ __forceinline__ void each_group(unsigned steps, const float2* first, Set&& set) {
+#pragma unroll
+    for (int j = 0; j < (N == 1 ? 1 : V); ++j) set(j, first[steps >> (3 * j) & 7u]);
 }
 template <int N> __device__ __forceinline__ float2 of_pair(const float2 (&v)[N], int j) { return N == 1 ? v[0] : v[j]; }
 template <int N> __device__ __forceinline__ void put(float2 (&v)[N], int j, float value) {
@@ -170,17 +190,17 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_norm_kernel(NormShape 
     Rows rows(s, r, p, lengths, p.b);
     int mine = p.active ? rows.of(p.lane) : 0;
     {
-        const Fetch fetch(mine);
         const uint4* from = x + p.at(s, p.b);
-        for (int i = 0; i < mine; ++i, from += step) fetch(i, [&](int k) { copy_async16(slot + k * pitch, from); });
-        fetch.end();
+        refill(0, mine, [](int) {}, [&](int i) { copy_async16(slot + i * pitch, from); from += step; });
     }
     float2 gamma[N], beta[N];
-    each_element<N, V>(s, p.vector, [&](int j, int channel, int) {
+    each_channel<N, V>(s, p.vector, [&](int j, int channel) {
         put(gamma, j, p.active && gammas ? NormIo<IO>::one(gammas, channel) : 1.0f);
         put(beta, j, p.active && betas ? NormIo<IO>::one(betas, channel) : 0.0f);
     });
     const bool whole = N == 1 || s.width % V == 0;            // a vector lies in one group
+    const unsigned steps = group_steps<N, V>(s, p.vector);
+    const int group = p.column * V / s.width;                 // of the block, that of the first element
     const Divisor width(whole ? s.width / V : s.width);
     int round = 0;
     for (int64_t b = p.b; b < s.B; b += r.instances, ++round) {
@@ -255,31 +275,28 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_norm_kernel(NormShape 
             __syncthreads();
         }
         float2 mean[N], scale[N];
-        each_element<N, V>(s, p.vector, [&](int j, int, int group) {
-            const float2 v = m.result[p.active ? group - p.first_group : 0];
+        each_group<N, V>(steps, m.result + group, [&](int j, float2 v) {
             put(mean, j, v.x);
             put(scale, j, v.y);
         });
 #pragma unroll
         for (int j = 0; j < N; ++j) scale[j] = mul2(scale[j], gamma[j]);
         // every slot, once used, takes the next instance's vector
-        const Rows next(s, r, p, lengths, b + r.instances);
-        const Fetch fetch(p.active ? next.of(p.lane) : 0);
+        const Rows next = lengths || b + r.instances >= s.B ? Rows(s, r, p, lengths, b + r.instances) : rows;
+        const int count = p.active ? next.of(p.lane) : 0;
         uint4* to = y + p.at(s, b);
         const uint4* from = x + p.at(s, b + r.instances);
-        auto refill = [&](int i) { fetch(i, [&](int k) { copy_async16(slot + k * pitch, from); }); from += step; };
-        for (int i = 0; i < mine; ++i, to += step) {
+        auto apply = [&](int i) {
             float2 f[P];
             NormIo<IO>::widen(slot[i * pitch], f);
 #pragma unroll
             for (int j = 0; j < P; ++j) f[j] = activate<ACT>(fma2(sub2(f[j], of_pair(mean, j)), of_pair(scale, j), of_pair(beta, j)));
             *to = NormIo<IO>::narrow(f);
-            refill(i);
-        }
-        for (int i = mine; i < fetch.count; ++i) refill(i);
-        fetch.end();
+            to += step;
+        };
+        refill(mine, count, apply, [&](int i) { copy_async16(slot + i * pitch, from); from += step; });
         rows = next;
-        mine = fetch.count;
+        mine = count;
     }
 }
 
@@ -301,17 +318,21 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
     Rows rows(s, r, p, lengths, p.b);
     int mine = p.active ? rows.of(p.lane) : 0;
     {
-        const Fetch fetch(mine);
-        int64_t at = p.at(s, p.b);
-        for (int i = 0; i < mine; ++i, at += step)
-            fetch(i, [&](int k) { copy_async16(slot + k * pitch, x + at); copy_async16(slot + k * pitch + second, dy + at); });
-        fetch.end();
+        const uint4 *from_x = x + p.at(s, p.b), *from_dy = dy + p.at(s, p.b);
+        refill(0, mine, [](int) {}, [&](int i) {
+            copy_async16(slot + i * pitch, from_x);
+            copy_async16(slot + i * pitch + second, from_dy);
+            from_x += step;
+            from_dy += step;
+        });
     }
     float2 gamma[N], beta[N];
-    each_element<N, V>(s, p.vector, [&](int j, int channel, int) {
+    each_channel<N, V>(s, p.vector, [&](int j, int channel) {
         put(gamma, j, p.active && gammas ? NormIo<IO>::one(gammas, channel) : 1.0f);
         put(beta, j, p.active && betas ? NormIo<IO>::one(betas, channel) : 0.0f);
     });
+    const unsigned steps = group_steps<N, V>(s, p.vector);
+    const int group = p.column * V / s.width;                 // of the block, that of the first element
     const int each = s.C / s.groups, channels = p.groups * each, row = p.columns * r.sums;
     const Divisor runs(s.T / r.run);
     float2* sums = m.side + blockDim.x * r.sums;              // a channel's, of this instance and of all so far
@@ -322,8 +343,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
     for (int64_t b = p.b; b < s.B; b += r.instances, ++round) {
         // z = (x - mean) * (rstd * gamma) + beta;  rstd comes to the sums of dz * (x - mean) at the end
         float2 mean[N], scale[N], rstd[N];
-        each_element<N, V>(s, p.vector, [&](int j, int, int group) {
-            const float2 v = p.active ? stats[b * s.groups + group] : make_float2(0.0f, 0.0f);
+        each_group<N, V>(steps, stats + b * s.groups + p.first_group + group, [&](int j, float2 v) {
             put(mean, j, v.x);
             put(rstd, j, v.y);
         });
@@ -423,8 +443,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
         }
         // dx = dz * (rstd * gamma) - (x - mean) * (rstd * rstd * second) - rstd * first
         float2 off1[N], off2[N];
-        each_element<N, V>(s, p.vector, [&](int j, int, int group) {
-            const float2 v = m.result[p.active ? group - p.first_group : 0];
+        each_group<N, V>(steps, m.result + group, [&](int j, float2 v) {
             put(off1, j, -v.x);
             put(off2, j, -v.y);
         });
@@ -433,26 +452,26 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
             off1[j] = mul2(off1[j], rstd[j]);
             off2[j] = mul2(mul2(off2[j], rstd[j]), rstd[j]);
         }
-        const Rows next(s, r, p, lengths, b + r.instances);
-        const Fetch fetch(p.active ? next.of(p.lane) : 0);
+        const Rows next = lengths || b + r.instances >= s.B ? Rows(s, r, p, lengths, b + r.instances) : rows;
+        const int count_next = p.active ? next.of(p.lane) : 0;
         uint4* to = dx + p.at(s, b);
-        int64_t at = p.at(s, b + r.instances);
-        auto refill = [&](int i) {
-            fetch(i, [&](int k) { copy_async16(slot + k * pitch, x + at); copy_async16(slot + k * pitch + second, dy + at); });
-            at += step;
-        };
-        for (int i = 0; i < mine; ++i, to += step) {
+        const uint4 *from_x = x + p.at(s, b + r.instances), *from_dy = dy + p.at(s, b + r.instances);
+        auto apply = [&](int i) {
             both(i);
             float2 f[P];
 #pragma unroll
             for (int j = 0; j < P; ++j) f[j] = fma2(xc[j], of_pair(off2, j), fma2(dz[j], of_pair(scale, j), of_pair(off1, j)));
             *to = NormIo<IO>::narrow(f);
-            refill(i);
-        }
-        for (int i = mine; i < fetch.count; ++i) refill(i);
-        fetch.end();
+            to += step;
+        };
+        refill(mine, count_next, apply, [&](int i) {
+            copy_async16(slot + i * pitch, from_x);
+            copy_async16(slot + i * pitch + second, from_dy);
+            from_x += step;
+            from_dy += step;
+        });
         rows = next;
-        mine = fetch.count;
+        mine = count_next;
     }
     float2* out = parts + (p.b * r.cluster + p.rank) * s.C + p.first_group * each;
     for (int c0 = 0; c0 < channels; c0 += teams)               // (each by the thread that added it up)
