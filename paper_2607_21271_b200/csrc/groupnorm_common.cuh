@@ -42,6 +42,13 @@ cudaError_t launch_warp_gradient(const NormShape& s, const WarpNorm& w, eql_dtyp
                                  const void* beta, const int32_t* lengths, const float* stats, void* dx, float* parts, cudaStream_t stream);
 
 // Units resident in shared memory (groupnorm_resident.cu): a unit is one instance's part of a block of groups.
+// e / d for e below 2^16 and d up to 2^16, by a reciprocal: ceil(2^32 / d).
+struct Divisor {
+    unsigned d, inverse;
+    __host__ __device__ Divisor() : d(1), inverse(0) {}
+    __host__ __device__ explicit Divisor(unsigned by) : d(by), inverse(by > 1 ? 0xffffffffu / by + 1 : 0) {}
+    __device__ __forceinline__ unsigned operator()(unsigned e) const { return d > 1 ? __umulhi(e, inverse) : e; }
+};
 struct ResidentNorm {
     bool supported;
     int groups, blocks;       // groups of a block, blocks of a row
@@ -50,6 +57,7 @@ struct ResidentNorm {
     int64_t rows;             // rows of a CTA
     int run, sums, share;     // backward: neighbouring elements summed up in a thread, sums of a vector, lanes that add up a channel
     int slot_bytes, side_offset, shared_bytes;
+    Divisor tuple, width, entry, runs;        // T; elements of a group; entries of a group in a row (its vectors, or elements); runs of a tuple
 };
 constexpr int kResidentShared = 220 * 1024;
 ResidentNorm resident_norm_plan(const NormShape& s, eql_dtype_t dtype, bool backward);
@@ -189,7 +197,7 @@ struct RunningMoments {
         }
     }
 };
-__device__ __forceinline__ float rstd_of(const Moments& v, float eps) { return 1.0f / sqrtf((v.n > 0.0f ? v.m2 / v.n : 0.0f) + eps); }
+__device__ __forceinline__ float rstd_of(const Moments& v, float eps) { return rsqrtf((v.n > 0.0f ? __fdividef(v.m2, v.n) : 0.0f) + eps); }
 
 __device__ __forceinline__ int64_t positions_of(const int32_t* lengths, int64_t b, int64_t S) {
     if (!lengths) return S;

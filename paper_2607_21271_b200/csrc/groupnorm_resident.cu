@@ -31,14 +31,15 @@ struct Post {
     int lane, lanes, rank;
     bool active;
     __device__ __forceinline__ Post(const NormShape& s, const ResidentNorm& r, int V) {
-        const unsigned unit = blockIdx.x / (unsigned)r.cluster, block = unit % (unsigned)r.blocks;
-        rank = blockIdx.x % (unsigned)r.cluster;
-        b = unit / (unsigned)r.blocks;
+        const unsigned unit = blockIdx.x / (unsigned)r.cluster, instance = unit / (unsigned)r.blocks, block = unit - instance * r.blocks;
+        rank = blockIdx.x - unit * r.cluster;
+        b = instance;
         first_group = block * r.groups;
         groups = min(r.groups, s.groups - first_group);
         columns = groups * s.width / V;
-        lanes = blockDim.x / (unsigned)columns;
-        lane = threadIdx.x / (unsigned)columns;
+        const Divisor by(columns);
+        lanes = by(blockDim.x);
+        lane = by(threadIdx.x);
         column = threadIdx.x - lane * columns;
         vector = first_group * s.width / V + column;
         active = lane < lanes;
@@ -58,13 +59,6 @@ struct Rows {
     }
     __device__ __forceinline__ int of(int lane) const { return each + (lane < extra ? 1 : 0); }
 };
-// e / d for e below 2^16 and d up to 2^16, by a reciprocal computed once: ceil(2^32 / d).
-struct Divisor {
-    unsigned d, inverse;
-    __device__ __forceinline__ explicit Divisor(unsigned by) : d(by), inverse(by > 1 ? 0xffffffffu / by + 1 : 0) {}
-    __device__ __forceinline__ unsigned operator()(unsigned e) const { return d > 1 ? __umulhi(e, inverse) : e; }
-};
-
 // Shared memory, behind the slots: results a group (float2), what the cluster's CTAs sent (for this instance and the one before:
 // [2][CTA][group] of three floats), and the room in which threads put their partial results side by side.
 struct Room {
@@ -115,34 +109,36 @@ __device__ __forceinline__ float warp_sum(float v) {
 }
 __device__ __forceinline__ float element(const float2* v, int j) { return j % 2 ? v[j / 2].y : v[j / 2].x; }
 
-// Mean and squared distances of a warp's entries, each of n values: the mean first, then the distances from it.  at(e) gives an entry's n
-// and its (mean, squared distances).
+// Mean and squared distances of a warp's entries, each of n values, `count` in all.  at(e) gives an entry's n and its (mean, squared
+// distances).  The entries' means are taken relative to the average of the lanes' first ones, which a single far value moves by no
+// more than a 32nd of what it moves its own entry's mean (or by its share, of fewer entries).
 template <typename At>
-__device__ __forceinline__ Moments moments_of(int entries, At&& at) {
+__device__ __forceinline__ Moments moments_of(float count, int entries, At&& at) {
     const int lane = threadIdx.x & 31;
-    float count = 0.0f, sum = 0.0f, m2 = 0.0f;
-    for (int e = lane; e < entries; e += 32) {
-        float n;
-        const float2 v = at(e, &n);
-        count += n;
-        sum = fmaf(n, v.x, sum);
+    float sum = 0.0f, m2 = 0.0f, n = 0.0f;
+    float2 v = make_float2(0.0f, 0.0f);
+    if (lane < entries) v = at(lane, &n);
+    const float middle = entries > 0 ? __fdividef(warp_sum(v.x), (float)min(entries, 32)) : 0.0f;
+    for (int e = lane; e < entries;) {
+        const float d = v.x - middle;
+        sum = fmaf(n, d, sum);
+        m2 += fmaf(n * d, d, v.y);
+        e += 32;
+        if (e < entries) v = at(e, &n);
     }
-    count = warp_sum(count);
-    const float mean = count > 0.0f ? warp_sum(sum) / count : 0.0f;
-    for (int e = lane; e < entries; e += 32) {
-        float n;
-        const float2 v = at(e, &n);
-        m2 += n > 0.0f ? fmaf(n * (v.x - mean), v.x - mean, v.y) : 0.0f;
-    }
-    return Moments{count, mean, warp_sum(m2)};
+    sum = warp_sum(sum);
+    m2 = warp_sum(m2);
+    const float mean = count > 0.0f ? __fdividef(sum, count) : 0.0f;
+    m2 -= sum * mean;
+    return Moments{count, middle + mean, m2 < 0.0f ? 0.0f : m2};
 }
 
 // The groups of a vector's elements, relative to its first element's: three bits each.
 template <int N, int V>
-__device__ __forceinline__ unsigned group_steps(const NormShape& s, int vector) {
+__device__ __forceinline__ unsigned group_steps(const NormShape& s, int in_group) {
     unsigned steps = 0;
     if (N > 1) {
-        int in_group = vector * V % s.width, step = 0;
+        int step = 0;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             steps |= step << (3 * j);
@@ -154,8 +150,9 @@ __device__ __forceinline__ unsigned group_steps(const NormShape& s, int vector) 
 // What belongs to the elements of a vector: N = 1 where they are of one channel (and so of one group), else a pair for each two.
 // set(element, channel) for every element, and set(element, group) with the steps above.
 template <int N, int V, typename Set>
-__device__ __forceinline__ void each_channel(const NormShape& s, int vector, Set&& set) {
-    int channel = vector * V / s.T, in_channel = vector * V - channel * s.T;
+__device__ __forceinline__ void each_channel(const NormShape& s, const ResidentNorm& r, const Post& p, Set&& set) {
+    int channel = r.tuple(p.column * V), in_channel = p.column * V - channel * s.T;
+    channel += p.first_group * (s.C / s.groups);
 #pragma unroll
     for (int j = 0; j < (N == 1 ? 1 : V); ++j) {
         set(j, channel);
@@ -194,14 +191,13 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_norm_kernel(NormShape 
         refill(0, mine, [](int) {}, [&](int i) { copy_async16(slot + i * pitch, from); from += step; });
     }
     float2 gamma[N], beta[N];
-    each_channel<N, V>(s, p.vector, [&](int j, int channel) {
+    each_channel<N, V>(s, r, p, [&](int j, int channel) {
         put(gamma, j, p.active && gammas ? NormIo<IO>::one(gammas, channel) : 1.0f);
         put(beta, j, p.active && betas ? NormIo<IO>::one(betas, channel) : 0.0f);
     });
     const bool whole = N == 1 || s.width % V == 0;            // a vector lies in one group
-    const unsigned steps = group_steps<N, V>(s, p.vector);
-    const int group = p.column * V / s.width;                 // of the block, that of the first element
-    const Divisor width(whole ? s.width / V : s.width);
+    const int group = r.width(p.column * V);                  // of the block, that of the first element
+    const unsigned steps = group_steps<N, V>(s, p.column * V - group * s.width);
     int round = 0;
     for (int64_t b = p.b; b < s.B; b += r.instances, ++round) {
         RunningMoments<P> moments;
@@ -216,18 +212,23 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_norm_kernel(NormShape 
         copies_wait<0>();
         for (int i = half; i < mine; ++i) add(i);
         if (whole) {                                          // the columns of a vector have as many values each
-            float mean = 0.0f, m2 = 0.0f;
+            float2 sum = moments.mean[0], squares = moments.m2[0];
 #pragma unroll
-            for (int j = 0; j < V; ++j) mean += element(moments.mean, j);
-            mean *= 1.0f / V;
+            for (int j = 1; j < P; ++j) sum = add2(sum, moments.mean[j]);
+            const float mean = (sum.x + sum.y) * (1.0f / V);
+            float2 off = sub2(moments.mean[0], pair(mean)), around = mul2(off, off);
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const float d = element(moments.mean, j) - mean;
-                m2 += fmaf(moments.rows * d, d, element(moments.m2, j));
+            for (int j = 1; j < P; ++j) {
+                off = sub2(moments.mean[j], pair(mean));
+                around = fma2(off, off, around);
+                squares = add2(squares, moments.m2[j]);
             }
+            squares = fma2(around, pair(moments.rows), squares);
+            const float m2 = squares.x + squares.y;
             if (p.groups == 1) {                              // every thread's: a warp's together
-                const Moments t = moments_of(32, [&](int, float* n) { *n = moments.rows * V; return make_float2(mean, m2); });
-                if ((threadIdx.x & 31) == 0) { m.side[2 * warp] = make_float2(t.mean, t.m2); m.side[2 * warp + 1].x = t.n; }
+                const float n = moments.rows * V, all = warp_sum(n), middle = all > 0.0f ? __fdividef(warp_sum(n * mean), all) : 0.0f;
+                const float around_all = warp_sum(fmaf(n * (mean - middle), mean - middle, m2));
+                if ((threadIdx.x & 31) == 0) { m.side[2 * warp] = make_float2(middle, around_all); m.side[2 * warp + 1].x = all; }
             } else {
                 m.side[threadIdx.x] = make_float2(mean, m2);
             }
@@ -239,15 +240,17 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_norm_kernel(NormShape 
         if (r.cluster > 1 && round == 0) ptx::cluster_wait(); // the other CTAs have started: their shared memory may be written
         for (int g = warp; g < p.groups; g += warps) {
             Moments t;
+            const float count = (float)rows.all * s.width;
             if (whole && p.groups == 1) {
-                t = moments_of(warps, [&](int e, float* n) { *n = m.side[2 * e + 1].x; return m.side[2 * e]; });
+                t = moments_of(count, warps, [&](int e, float* n) { *n = m.side[2 * e + 1].x; return m.side[2 * e]; });
             } else {
                 // entries of a lane of rows: the group's vectors, or where they cross its border its elements
                 const int per = whole ? 1 : V, row = p.columns * per;
-                t = moments_of(min(p.lanes, rows.all) * (int)width.d, [&](int e, float* n) {
-                    const int l = width(e);
-                    *n = (float)(rows.of(l) * (V / per));
-                    return m.side[l * row + (g - l) * (int)width.d + e];
+                const float more = (float)((rows.each + 1) * (V / per)), fewer = (float)(rows.each * (V / per));
+                t = moments_of(count, min(p.lanes, rows.all) * (int)r.entry.d, [&](int e, float* n) {
+                    const int l = r.entry(e);
+                    *n = l < rows.extra ? more : fewer;
+                    return m.side[l * row + (g - l) * (int)r.entry.d + e];
                 });
             }
             if (r.cluster > 1) {
@@ -327,14 +330,13 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
         });
     }
     float2 gamma[N], beta[N];
-    each_channel<N, V>(s, p.vector, [&](int j, int channel) {
+    each_channel<N, V>(s, r, p, [&](int j, int channel) {
         put(gamma, j, p.active && gammas ? NormIo<IO>::one(gammas, channel) : 1.0f);
         put(beta, j, p.active && betas ? NormIo<IO>::one(betas, channel) : 0.0f);
     });
-    const unsigned steps = group_steps<N, V>(s, p.vector);
-    const int group = p.column * V / s.width;                 // of the block, that of the first element
+    const int group = r.width(p.column * V);                  // of the block, that of the first element
+    const unsigned steps = group_steps<N, V>(s, p.column * V - group * s.width);
     const int each = s.C / s.groups, channels = p.groups * each, row = p.columns * r.sums;
-    const Divisor runs(s.T / r.run);
     float2* sums = m.side + blockDim.x * r.sums;              // a channel's, of this instance and of all so far
     float2* total = sums + r.groups * each;
     const int teams = blockDim.x / (unsigned)r.share, team = threadIdx.x / (unsigned)r.share;
@@ -395,14 +397,14 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
         }
         __syncthreads();
         // Channels: `share` lanes each, over the lanes of rows and the runs of the tuple.
-        const int entries = min(p.lanes, rows.all) * (int)runs.d;
+        const int entries = min(p.lanes, rows.all) * (int)r.runs.d;
         for (int c0 = 0; c0 < channels; c0 += teams) {
             const int c = c0 + team;
             float2 v = make_float2(0.0f, 0.0f);
             if (c < channels)
                 for (int e = threadIdx.x - team * r.share; e < entries; e += r.share) {
-                    const int l = runs(e);
-                    v = add2(v, m.side[l * row + (c - l) * (int)runs.d + e]);
+                    const int l = r.runs(e);
+                    v = add2(v, m.side[l * row + (c - l) * (int)r.runs.d + e]);
                 }
             for (int d = r.share >> 1; d > 0; d >>= 1) {
                 v.x += __shfl_xor_sync(0xffffffffu, v.x, d);
@@ -415,7 +417,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
         }
         __syncthreads();
         if (r.cluster > 1 && round == 0) ptx::cluster_wait();
-        const float count = (float)positions_of(lengths, b, s.S) * s.width, share = count > 0.0f ? 1.0f / count : 0.0f;
+        const float count = (float)positions_of(lengths, b, s.S) * s.width, share = count > 0.0f ? __fdividef(1.0f, count) : 0.0f;
         for (int g = warp; g < p.groups; g += blockDim.x >> 5) {
             float2 v = make_float2(0.0f, 0.0f);
             for (int c = lane; c < each; c += 32) {
@@ -481,15 +483,8 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
 }  // namespace
 
 constexpr int kFewThreads = 256, kManyForward = 1024, kManyBackward = 512;
-#ifndef TUNE_FWD_CTAS
-#define TUNE_FWD_CTAS 4
-#define TUNE_BWD_CTAS1 3
-#define TUNE_BWD_CTAS 2
-#define TUNE_SHARED 74
-#define TUNE_PERSIST 1
-#endif
 // CTAs of 256 threads to an SM, by the registers that the kernels then may use.
-constexpr int kForwardCtas = TUNE_FWD_CTAS, kGradientCtasTuple = TUNE_BWD_CTAS1, kGradientCtas = TUNE_BWD_CTAS;
+constexpr int kForwardCtas = 4, kGradientCtasTuple = 3, kGradientCtas = 2;
 
 ResidentNorm resident_norm_plan(const NormShape& s, eql_dtype_t dtype, bool backward) {
     ResidentNorm r{};
@@ -509,6 +504,10 @@ ResidentNorm resident_norm_plan(const NormShape& s, eql_dtype_t dtype, bool back
     r.blocks = (s.groups + r.groups - 1) / r.groups;
     r.run = s.T % V == 0 ? V : V % s.T == 0 ? s.T : 1;
     r.sums = V / r.run;
+    r.tuple = Divisor(s.T);
+    r.width = Divisor(s.width);
+    r.entry = Divisor(s.width % V == 0 ? s.width / V : s.width);
+    r.runs = Divisor(s.T / r.run);
     const int channels = r.groups * (s.C / s.groups), lanes = (int)(r.threads / columns);
     const int side = backward ? r.threads * r.sums + 2 * channels : s.width % V == 0 ? r.threads : r.threads * V;
     for (r.cluster = 1; r.cluster <= kMaxCluster; r.cluster *= 2) {
@@ -521,8 +520,9 @@ ResidentNorm resident_norm_plan(const NormShape& s, eql_dtype_t dtype, bool back
             r.side_offset += r.slot_bytes;
             r.shared_bytes = (int)all;
             r.supported = true;
-            // larger clusters until three CTAs fit an SM, and every SM has one or a thread has no more than four vectors
-            if (all <= TUNE_SHARED * 1024 && (s.B * r.blocks * r.cluster >= kNumSMs || slots <= 4)) break;
+            // One CTA where two of them fit an SM; else larger clusters until three do, and every SM has one or a thread has no more than
+            // four vectors.  (Backward, one CTA of 83 KB / clusters of two with 42 KB: 128 x 197 x 768 bfloat16 38 / 49 us.)
+            if (all <= (r.cluster == 1 ? 112 : 74) * 1024 && (s.B * r.blocks * r.cluster >= kNumSMs || slots <= 4)) break;
         }
         if (r.cluster == kMaxCluster) break;
     }
@@ -537,7 +537,7 @@ ResidentNorm resident_norm_plan(const NormShape& s, eql_dtype_t dtype, bool back
     together = together * kNumSMs / (r.blocks * r.cluster);
     if (together < 1) together = 1;
     r.instances = (int)s.B;
-    if (TUNE_PERSIST && r.cluster == 1 && together < s.B) {
+    if (r.cluster == 1 && together < s.B) {
         const int64_t rounds = (s.B + together - 1) / together;
         r.instances = (int)((s.B + rounds - 1) / rounds);
     }
