@@ -416,7 +416,7 @@ eql_status_t eqlinear_adamw_clip(eqlinear_adamw_t opt, float max_norm, const flo
 
 /* One step over all tensors (one kernel); uses up what eqlinear_adamw_clip left.
  *   lr         >= 0, used unless lr_device is given: a device float, read when the kernel runs (schedules in captured graphs)
- *   beta1, beta2 in [0, 1);  eps > 0
+ *   beta1, beta2 in [0, 1);  eps at least 2^-126
  * The step number lives on the device and advances by itself, so a captured step can be replayed. */
 eql_status_t eqlinear_adamw_step(eqlinear_adamw_t opt, double lr, double beta1, double beta2, double eps,
                                  const float* lr_device, void* stream);

@@ -10,11 +10,13 @@
 #include <cuda_fp8.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdlib>
 #include <new>
 
 #include "eql_internal.h"
+#include "packed.cuh"
 #include "ptx_sm100.cuh"
 
 namespace eql {
@@ -23,7 +25,8 @@ namespace {
 constexpr int kBlock = 256;                 // elements that share a scale: one warp's
 constexpr int kAdamThreads = 256;
 constexpr int kChunk = kBlock * (kAdamThreads / 32);
-constexpr int kNormCtasPerSm = 4, kStepCtasPerSm = 3;
+constexpr int kNormCtasPerSm = 4, kStepCtasPerSm = 3;      // resident together, by their registers
+constexpr int kNormUnroll = 4;              // chunks of gradients that a warp has on their way
 constexpr int kMaxNormCtas = 1024;
 constexpr float kE4m3Max = 448.0f, kE5m2Max = 57344.0f, kE5m2Least = 0x1p-16f, kTiny = 0x1p-100f;
 
@@ -57,6 +60,7 @@ struct Layout {
 // What a step has in every element's formula (host: rounded once from double).
 struct Rates {
     float lr, beta1, one_minus_beta1, beta2, one_minus_beta2, eps;
+    float one;                // 1: see adamw_kernel
     double log_beta1, log_beta2;
     const float* lr_device;
 };
@@ -73,12 +77,17 @@ __device__ __forceinline__ uint4 load_raw4(const void* base, int64_t at, int dty
 __device__ __forceinline__ float widen16(uint32_t bits, int dtype) {
     return dtype == EQL_FP16 ? __half2float(__ushort_as_half((unsigned short)bits)) : __uint_as_float(bits << 16);
 }
-__device__ __forceinline__ void widen4(const uint4& u, int dtype, float* f) {
+__device__ __forceinline__ float2 widen_pair(uint32_t u, int dtype) {
+    if (dtype == EQL_FP16) return __half22float2(*reinterpret_cast<const __half2*>(&u));
+    return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+}
+__device__ __forceinline__ void widen4(const uint4& u, int dtype, float2* f) {
     if (dtype == EQL_FP32) {
-        f[0] = __uint_as_float(u.x); f[1] = __uint_as_float(u.y); f[2] = __uint_as_float(u.z); f[3] = __uint_as_float(u.w);
+        f[0] = make_float2(__uint_as_float(u.x), __uint_as_float(u.y));
+        f[1] = make_float2(__uint_as_float(u.z), __uint_as_float(u.w));
     } else {
-        f[0] = widen16(u.x & 0xffffu, dtype); f[1] = widen16(u.x >> 16, dtype);
-        f[2] = widen16(u.y & 0xffffu, dtype); f[3] = widen16(u.y >> 16, dtype);
+        f[0] = widen_pair(u.x, dtype);
+        f[1] = widen_pair(u.y, dtype);
     }
 }
 __device__ __forceinline__ float load_one(const void* base, int64_t at, int dtype) {
@@ -88,12 +97,19 @@ __device__ __forceinline__ float load_one(const void* base, int64_t at, int dtyp
 __device__ __forceinline__ uint32_t narrow16(float v, int dtype) {
     return dtype == EQL_FP16 ? __half_as_ushort(__float2half_rn(v)) : __bfloat16_as_ushort(__float2bfloat16_rn(v));
 }
-__device__ __forceinline__ void store4(void* base, int64_t at, int dtype, const float* f) {
+__device__ __forceinline__ uint32_t narrow_pair(float2 f, int dtype) {
+    if (dtype == EQL_FP16) {
+        const __half2 h = __floats2half2_rn(f.x, f.y);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+    const __nv_bfloat162 h = __floats2bfloat162_rn(f.x, f.y);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ void store4(void* base, int64_t at, int dtype, const float2* f) {
     if (dtype == EQL_FP32)
-        __stcs(reinterpret_cast<float4*>(static_cast<float*>(base) + at), make_float4(f[0], f[1], f[2], f[3]));
+        __stcs(reinterpret_cast<float4*>(static_cast<float*>(base) + at), make_float4(f[0].x, f[0].y, f[1].x, f[1].y));
     else
-        __stcs(reinterpret_cast<uint2*>(static_cast<uint16_t*>(base) + at),
-               make_uint2(narrow16(f[0], dtype) | narrow16(f[1], dtype) << 16, narrow16(f[2], dtype) | narrow16(f[3], dtype) << 16));
+        __stcs(reinterpret_cast<uint2*>(static_cast<uint16_t*>(base) + at), make_uint2(narrow_pair(f[0], dtype), narrow_pair(f[1], dtype)));
 }
 __device__ __forceinline__ void store_one(void* base, int64_t at, int dtype, float f) {
     if (dtype == EQL_FP32) static_cast<float*>(base)[at] = f;
@@ -101,33 +117,35 @@ __device__ __forceinline__ void store_one(void* base, int64_t at, int dtype, flo
 }
 
 template <__nv_fp8_interpretation_t KIND>
-__device__ __forceinline__ void decode4(uint32_t codes, float scale, float* f) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(codes >> (16 * h)), KIND);
-        const float2 w = __half22float2(__half2(r));
-        f[2 * h] = __fmul_rn(w.x, scale);
-        f[2 * h + 1] = __fmul_rn(w.y, scale);
-    }
+__device__ __forceinline__ float2 decode_pair(uint32_t codes, float2 scale) {
+    const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)codes, KIND);
+    return mul2(__half22float2(__half2(r)), scale);
 }
 template <__nv_fp8_interpretation_t KIND>
-__device__ __forceinline__ uint32_t encode4(const float* q) {
-    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(q[0], q[1]), __NV_SATFINITE, KIND);
-    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(q[2], q[3]), __NV_SATFINITE, KIND);
+__device__ __forceinline__ void decode4(uint32_t codes, float2 scale, float2* f) {
+    f[0] = decode_pair<KIND>(codes & 0xffffu, scale);
+    f[1] = decode_pair<KIND>(codes >> 16, scale);
+}
+template <__nv_fp8_interpretation_t KIND>
+__device__ __forceinline__ uint32_t encode4(const float2* q) {
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(q[0], __NV_SATFINITE, KIND);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(q[1], __NV_SATFINITE, KIND);
     return lo | hi << 16;
 }
 
-__device__ __forceinline__ float warp_max(float v) {
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
-    return v;
-}
+// The largest of a warp's values, which are not negative: their bits are in the order of the values, NaN last.
+__device__ __forceinline__ float warp_max(float v) { return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v))); }
+__device__ __forceinline__ float& half_of(float2* v, int j) { return j % 2 ? v[j / 2].y : v[j / 2].x; }
 
 // The step, states of BITS bits.  The moments are computed by separately rounded operations: in 8 bits, what lies next to the border
-// of two codes goes by their last bit, and a plain program has to come to the same codes.  The denominator may be a few float
+// of two codes goes by their last bit, and a plain program has to come to the same codes.  (The assembler makes one fused operation of
+// a packed product and a packed sum, their rounding modes notwithstanding; a sum written as a * 1 + b, with a 1 that it does not
+// know, is left alone.)  The denominator may be a few float
 // roundings off (approximate square root and division, about 2^-22): it moves the parameter by lr times that.
-template <int BITS>
-__global__ void __launch_bounds__(kAdamThreads) adamw_kernel(char* ws, Layout lay, Rates r) {
+// GRAD, PARAM: the type that all tensors have there, or kMixed.
+constexpr int kMixed = -1;
+template <int BITS, int GRAD, int PARAM>
+__global__ void __launch_bounds__(kAdamThreads, kStepCtasPerSm) adamw_kernel(char* ws, Layout lay, Rates r) {
     ptx::grid_handover();
     Control* control = reinterpret_cast<Control*>(ws);
     const Tensor* tensors = reinterpret_cast<const Tensor*>(ws + lay.tensors);
@@ -135,32 +153,43 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(char* ws, Layout la
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int32_t skip = control->skip;
     if (!skip) {
-        const float factor = control->factor;
+        const float2 factor = pair(control->factor);
         const double t = (double)(control->step + 1);
         const float lr = r.lr_device ? *r.lr_device : r.lr;
         const float correction1 = -expm1f((float)(t * r.log_beta1)), correction2 = -expm1f((float)(t * r.log_beta2));
-        const float root2 = rsqrtf(correction2);
+        const float2 root2 = pair(rsqrtf(correction2)), eps = pair(r.eps);
+        const float2 beta1 = pair(r.beta1), new1 = pair(r.one_minus_beta1), beta2 = pair(r.beta2), new2 = pair(r.one_minus_beta2), one = pair(r.one);
         const int64_t begin = lay.n_chunks * blockIdx.x / gridDim.x, end = lay.n_chunks * (blockIdx.x + 1) / gridDim.x;
-        int32_t which = -1;
+        int32_t which = -1, next = begin < end ? chunk_tensor[begin] : 0;
         Tensor x{};
+        float2 keep{}, size{};
         for (int64_t c = begin; c < end; ++c) {
-            const int32_t now = chunk_tensor[c];
-            if (now != which) { x = tensors[now]; which = now; }
+            const int32_t now = next;
+            if (c + 1 < end) next = chunk_tensor[c + 1];
+            if (now != which) {
+                x = tensors[now];
+                which = now;
+                const float rate = lr * x.lr_scale;
+                keep = pair(1.0f - rate * x.weight_decay);
+                size = pair(-rate / correction1);
+            }
+            const int grad_dtype = GRAD == kMixed ? x.grad_dtype : GRAD, param_dtype = PARAM == kMixed ? x.param_dtype : PARAM;
             const int64_t base = (c - x.first_chunk) * kChunk + warp * kBlock;
             const int64_t left = x.numel - base;
             if (left <= 0) continue;
-            const float rate = lr * x.lr_scale, keep = 1.0f - rate * x.weight_decay, size = rate / correction1;
             const bool full = left >= kBlock;
-            float g[8], m[8], v[8], p[8];
+            float2 g[4], m[4], v[4], p[4];
             const void* from = x.master ? (const void*)x.master : (const void*)x.param;
-            const int from_dtype = x.master ? (int)EQL_FP32 : x.param_dtype;
+            const int from_dtype = x.master ? (int)EQL_FP32 : param_dtype;
             const int64_t block = base / kBlock;
+            float2 ms{}, vs{};
+            if (BITS == 8) { ms = pair(x.m_scale[block]); vs = pair(x.v_scale[block]); }
             if (full) {
                 uint4 rg[2], rp[2], rm[2], rv[2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int64_t at = base + h * 128 + lane * 4;
-                    rg[h] = load_raw4(x.grad, at, x.grad_dtype);
+                    rg[h] = load_raw4(x.grad, at, grad_dtype);
                     rp[h] = load_raw4(from, at, from_dtype);
                     if (BITS == 32) {
                         rm[h] = load_raw4(x.m, at, EQL_FP32);
@@ -170,81 +199,83 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(char* ws, Layout la
                         rv[h].x = __ldcs(reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(x.v) + at));
                     }
                 }
-                const float ms = BITS == 8 ? x.m_scale[block] : 0.0f, vs = BITS == 8 ? x.v_scale[block] : 0.0f;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    widen4(rg[h], x.grad_dtype, g + 4 * h);
-                    widen4(rp[h], from_dtype, p + 4 * h);
+                    widen4(rg[h], grad_dtype, g + 2 * h);
+                    widen4(rp[h], from_dtype, p + 2 * h);
                     if (BITS == 32) {
-                        widen4(rm[h], EQL_FP32, m + 4 * h);
-                        widen4(rv[h], EQL_FP32, v + 4 * h);
+                        widen4(rm[h], EQL_FP32, m + 2 * h);
+                        widen4(rv[h], EQL_FP32, v + 2 * h);
                     } else {
-                        decode4<__NV_E4M3>(rm[h].x, ms, m + 4 * h);
-                        decode4<__NV_E5M2>(rv[h].x, vs, v + 4 * h);
+                        decode4<__NV_E4M3>(rm[h].x, ms, m + 2 * h);
+                        decode4<__NV_E5M2>(rv[h].x, vs, v + 2 * h);
                     }
                 }
             } else {
-                const float ms = BITS == 8 ? x.m_scale[block] : 0.0f, vs = BITS == 8 ? x.v_scale[block] : 0.0f;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    g[j] = m[j] = v[j] = p[j] = 0.0f;
+                    half_of(g, j) = half_of(m, j) = half_of(v, j) = half_of(p, j) = 0.0f;
                     const int64_t at = base + lane_element(lane, j);
                     if (at >= x.numel) continue;
-                    g[j] = load_one(x.grad, at, x.grad_dtype);
-                    p[j] = load_one(from, at, from_dtype);
+                    half_of(g, j) = load_one(x.grad, at, grad_dtype);
+                    half_of(p, j) = load_one(from, at, from_dtype);
                     if (BITS == 32) {
-                        m[j] = static_cast<const float*>(x.m)[at];
-                        v[j] = static_cast<const float*>(x.v)[at];
+                        half_of(m, j) = static_cast<const float*>(x.m)[at];
+                        half_of(v, j) = static_cast<const float*>(x.v)[at];
                     } else {
-                        float f[4];
-                        decode4<__NV_E4M3>(static_cast<const uint8_t*>(x.m)[at], ms, f);
-                        m[j] = f[0];
-                        decode4<__NV_E5M2>(static_cast<const uint8_t*>(x.v)[at], vs, f);
-                        v[j] = f[0];
+                        half_of(m, j) = decode_pair<__NV_E4M3>(static_cast<const uint8_t*>(x.m)[at], ms).x;
+                        half_of(v, j) = decode_pair<__NV_E5M2>(static_cast<const uint8_t*>(x.v)[at], vs).x;
                     }
                 }
             }
             float most_m = 0.0f, most_v = 0.0f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float gs = __fmul_rn(g[j], factor);
-                m[j] = __fadd_rn(__fmul_rn(m[j], r.beta1), __fmul_rn(gs, r.one_minus_beta1));
-                v[j] = __fadd_rn(__fmul_rn(v[j], r.beta2), __fmul_rn(__fmul_rn(gs, gs), r.one_minus_beta2));
-                most_m = fmaxf(most_m, fabsf(m[j]));
-                most_v = fmaxf(most_v, v[j]);
-                float root;
-                asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(v[j]));
-                p[j] = p[j] * keep - __fdividef(size * m[j], root * root2 + r.eps);
+            for (int j = 0; j < 4; ++j) {
+                const float2 gs = mul2(g[j], factor);
+                m[j] = fma2(mul2(m[j], beta1), one, mul2(gs, new1));
+                v[j] = fma2(mul2(v[j], beta2), one, mul2(mul2(gs, gs), new2));
+                if (BITS == 8) {
+                    most_m = fmaxf(most_m, fmaxf(fabsf(m[j].x), fabsf(m[j].y)));
+                    most_v = fmaxf(most_v, fmaxf(v[j].x, v[j].y));
+                }
+                float2 root;
+                asm("sqrt.approx.f32 %0, %1;" : "=f"(root.x) : "f"(v[j].x));
+                asm("sqrt.approx.f32 %0, %1;" : "=f"(root.y) : "f"(v[j].y));
+                p[j] = fma2(mul2(size, m[j]), reciprocal(fma2(root, root2, eps)), mul2(p[j], keep));
             }
-            float qm[8], qv[8];
+            float2 qm[4], qv[4];
             if (BITS == 8) {
                 most_m = warp_max(most_m);
                 most_v = warp_max(most_v);
-                const bool fine_m = most_m >= kTiny, fine_v = most_v >= kTiny;
-                const float im = fine_m ? __fdiv_rn(kE4m3Max, most_m) : 0.0f, iv = fine_v ? __fdiv_rn(kE5m2Max, most_v) : 0.0f;
+                const bool fine_m = !(most_m < kTiny), fine_v = !(most_v < kTiny);
+                // the block's four divisions, each in another lane: the inverse scales of m and v, and the scales
+                const bool of_v = lane & 1, scale = lane & 2;
+                const float most = of_v ? most_v : most_m, top = of_v ? kE5m2Max : kE4m3Max;
+                const float ratio = (of_v ? fine_v : fine_m) ? __fdiv_rn(scale ? most : top, scale ? top : most) : 0.0f;
+                const float2 im = pair(__shfl_sync(0xffffffffu, ratio, 0)), iv = pair(__shfl_sync(0xffffffffu, ratio, 1));
+                const float least = fine_v ? kE5m2Least : 0.0f;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    qm[j] = __fmul_rn(m[j], im);
-                    qv[j] = __fmul_rn(v[j], iv);
-                    if (fine_v && v[j] > 0.0f) qv[j] = fmaxf(qv[j], kE5m2Least);
+                for (int j = 0; j < 4; ++j) {
+                    qm[j] = mul2(m[j], im);
+                    qv[j] = mul2(v[j], iv);
+                    if (v[j].x > 0.0f) qv[j].x = fmaxf(qv[j].x, least);
+                    if (v[j].y > 0.0f) qv[j].y = fmaxf(qv[j].y, least);
                 }
-                if (lane == 0) {
-                    x.m_scale[block] = fine_m ? __fdiv_rn(most_m, kE4m3Max) : 0.0f;
-                    x.v_scale[block] = fine_v ? __fdiv_rn(most_v, kE5m2Max) : 0.0f;
-                }
+                if (lane == 2) x.m_scale[block] = ratio;
+                if (lane == 3) x.v_scale[block] = ratio;
             }
             if (full) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int64_t at = base + h * 128 + lane * 4;
-                    if (x.master) store4(x.master, at, EQL_FP32, p + 4 * h);
-                    store4(x.param, at, x.param_dtype, p + 4 * h);
+                    if (x.master) store4(x.master, at, EQL_FP32, p + 2 * h);
+                    store4(x.param, at, param_dtype, p + 2 * h);
                     if (BITS == 32) {
-                        store4(x.m, at, EQL_FP32, m + 4 * h);
-                        store4(x.v, at, EQL_FP32, v + 4 * h);
+                        store4(x.m, at, EQL_FP32, m + 2 * h);
+                        store4(x.v, at, EQL_FP32, v + 2 * h);
                     } else {
-                        __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(x.m) + at), encode4<__NV_E4M3>(qm + 4 * h));
-                        __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(x.v) + at), encode4<__NV_E5M2>(qv + 4 * h));
+                        __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(x.m) + at), encode4<__NV_E4M3>(qm + 2 * h));
+                        __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(x.v) + at), encode4<__NV_E5M2>(qv + 2 * h));
                     }
                 }
             } else {
@@ -252,14 +283,14 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(char* ws, Layout la
                 for (int j = 0; j < 8; ++j) {
                     const int64_t at = base + lane_element(lane, j);
                     if (at >= x.numel) continue;
-                    if (x.master) x.master[at] = p[j];
-                    store_one(x.param, at, x.param_dtype, p[j]);
+                    if (x.master) x.master[at] = half_of(p, j);
+                    store_one(x.param, at, param_dtype, half_of(p, j));
                     if (BITS == 32) {
-                        static_cast<float*>(x.m)[at] = m[j];
-                        static_cast<float*>(x.v)[at] = v[j];
+                        static_cast<float*>(x.m)[at] = half_of(m, j);
+                        static_cast<float*>(x.v)[at] = half_of(v, j);
                     } else {
-                        static_cast<uint8_t*>(x.m)[at] = __nv_cvt_float_to_fp8(qm[j], __NV_SATFINITE, __NV_E4M3);
-                        static_cast<uint8_t*>(x.v)[at] = __nv_cvt_float_to_fp8(qv[j], __NV_SATFINITE, __NV_E5M2);
+                        static_cast<uint8_t*>(x.m)[at] = __nv_cvt_float_to_fp8(half_of(qm, j), __NV_SATFINITE, __NV_E4M3);
+                        static_cast<uint8_t*>(x.v)[at] = __nv_cvt_float_to_fp8(half_of(qv, j), __NV_SATFINITE, __NV_E5M2);
                     }
                 }
             }
@@ -303,39 +334,53 @@ __global__ void __launch_bounds__(kAdamThreads) grad_norm_kernel(char* ws, Layou
     __shared__ bool last;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t begin = lay.n_chunks * blockIdx.x / gridDim.x, end = lay.n_chunks * (blockIdx.x + 1) / gridDim.x;
-    double sum = 0.0;
-    int32_t which = -1;
-    const void* grad = nullptr;
-    int64_t numel = 0, first = 0;
-    int dtype = 0;
-    for (int64_t c = begin; c < end; ++c) {
-        const int32_t now = chunk_tensor[c];
-        if (now != which) {
-            which = now;
-            grad = tensors[now].grad; numel = tensors[now].numel; first = tensors[now].first_chunk; dtype = tensors[now].grad_dtype;
+    double sums[4] = {};
+    auto add = [&](const uint4& u, int dtype) {
+        float2 f[2];
+        widen4(u, dtype, f);
+        sums[0] = fma((double)f[0].x, (double)f[0].x, sums[0]);
+        sums[1] = fma((double)f[0].y, (double)f[0].y, sums[1]);
+        sums[2] = fma((double)f[1].x, (double)f[1].x, sums[2]);
+        sums[3] = fma((double)f[1].y, (double)f[1].y, sums[3]);
+    };
+    int64_t c = begin;
+    while (c < end) {
+        const int32_t which = chunk_tensor[c];
+        const void* grad = tensors[which].grad;
+        const int64_t numel = tensors[which].numel;
+        const int dtype = tensors[which].grad_dtype;
+        // this tensor's chunks, several whole ones at a time
+        int64_t base = (c - tensors[which].first_chunk) * kChunk + warp * kBlock;
+        const int64_t mine = min(end - c, (numel - base + warp * kBlock + kChunk - 1) / kChunk);
+        int64_t k = 0;
+        for (; k + kNormUnroll <= mine && base + (kNormUnroll - 1) * kChunk + kBlock <= numel; k += kNormUnroll, base += kNormUnroll * kChunk) {
+            uint4 u[kNormUnroll][2];
+#pragma unroll
+            for (int i = 0; i < kNormUnroll; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) u[i][h] = load_raw4(grad, base + i * kChunk + h * 128 + lane * 4, dtype);
+#pragma unroll
+            for (int i = 0; i < kNormUnroll; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) add(u[i][h], dtype);
         }
-        const int64_t base = (c - first) * kChunk + warp * kBlock;
-        if (numel - base >= kBlock) {
-            uint4 u[2];
+        for (; k < mine; ++k, base += kChunk) {
+            if (numel - base >= kBlock) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) u[h] = load_raw4(grad, base + h * 128 + lane * 4, dtype);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float f[4];
-                widen4(u[h], dtype, f);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) sum = fma((double)f[j], (double)f[j], sum);
-            }
-        } else {
-            for (int j = 0; j < 8; ++j) {
-                const int64_t at = base + lane_element(lane, j);
-                if (at < numel) {
-                    const double f = load_one(grad, at, dtype);
-                    sum = fma(f, f, sum);
+                for (int h = 0; h < 2; ++h) add(load_raw4(grad, base + h * 128 + lane * 4, dtype), dtype);
+            } else {
+                for (int j = 0; j < 8; ++j) {
+                    const int64_t at = base + lane_element(lane, j);
+                    if (at < numel) {
+                        const double f = load_one(grad, at, dtype);
+                        sums[0] = fma(f, f, sums[0]);
+                    }
                 }
             }
         }
+        c += mine;
     }
+    double sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
     sum = cta_sum(sum, shared);
     if (threadIdx.x == 0) {
         partials[blockIdx.x] = sum;
@@ -435,6 +480,7 @@ bool ranges_clash(Range* ranges, int n) {
 // The host object behind eqlinear_adamw_t.
 struct eqlinear_adamw_s {
     int device, num_sms, state_bits;
+    int grad_dtype, param_dtype;      // all tensors', or kMixed
     char* ws;
     eql::Layout lay;
 };
@@ -442,6 +488,18 @@ struct eqlinear_adamw_s {
 namespace {
 
 using namespace eql;
+
+using StepKernel = void (*)(char*, Layout, Rates);
+template <int BITS, int GRAD>
+StepKernel step_kernel(int param_dtype) {
+    return param_dtype == EQL_FP32 ? adamw_kernel<BITS, GRAD, EQL_FP32> : param_dtype == EQL_FP16 ? adamw_kernel<BITS, GRAD, EQL_FP16> : adamw_kernel<BITS, GRAD, EQL_BF16>;
+}
+template <int BITS>
+StepKernel step_kernel(int grad_dtype, int param_dtype) {
+    if (grad_dtype == kMixed || param_dtype == kMixed) return adamw_kernel<BITS, kMixed, kMixed>;
+    return grad_dtype == EQL_FP32 ? step_kernel<BITS, EQL_FP32>(param_dtype) : grad_dtype == EQL_FP16 ? step_kernel<BITS, EQL_FP16>(param_dtype)
+                                                                                                    : step_kernel<BITS, EQL_BF16>(param_dtype);
+}
 
 eql_status_t check_optimiser(eqlinear_adamw_t opt) {
     if (!opt) return EQL_ERR_INVALID_ARG;
@@ -507,8 +565,12 @@ eql_status_t eqlinear_adamw(eqlinear_adamw_t* opt, const eql_adamw_tensor_t* ten
     if (e == cudaSuccess) e = cudaStreamSynchronize(s);
     std::free(image);
     if (e != cudaSuccess) return EQL_ERR_CUDA;
-    eqlinear_adamw_s* o = new (std::nothrow) eqlinear_adamw_s{dev, sms, state_bits, (char*)workspace, lay};
+    eqlinear_adamw_s* o = new (std::nothrow) eqlinear_adamw_s{dev, sms, state_bits, tensors[0].grad_dtype, tensors[0].param_dtype, (char*)workspace, lay};
     if (!o) return EQL_ERR_INVALID_ARG;
+    for (int i = 1; i < count; ++i) {
+        if (tensors[i].grad_dtype != o->grad_dtype) o->grad_dtype = kMixed;
+        if (tensors[i].param_dtype != o->param_dtype) o->param_dtype = kMixed;
+    }
     *opt = o;
     return EQL_OK;
 }
@@ -527,13 +589,13 @@ eql_status_t eqlinear_adamw_clip(eqlinear_adamw_t opt, float max_norm, const flo
 eql_status_t eqlinear_adamw_step(eqlinear_adamw_t opt, double lr, double beta1, double beta2, double eps, const float* lr_device, void* stream) {
     if (eql_status_t st = check_optimiser(opt); st != EQL_OK) return st;
     if (!(lr >= 0.0) || !std::isfinite(lr) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0)) return EQL_ERR_INVALID_ARG;
-    if (!((float)eps > 0.0f) || !std::isfinite((float)eps)) return EQL_ERR_INVALID_ARG;
+    if (!((float)eps >= FLT_MIN) || !std::isfinite((float)eps)) return EQL_ERR_INVALID_ARG;
     if (!aligned(lr_device, 4)) return EQL_ERR_ALIGNMENT;
-    const Rates r{(float)lr, (float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps, std::log(beta1), std::log(beta2), lr_device};
+    const Rates r{(float)lr, (float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps, 1.0f, std::log(beta1), std::log(beta2), lr_device};
     const int64_t most = (int64_t)opt->num_sms * kStepCtasPerSm;
     const unsigned grid = (unsigned)std::max<int64_t>(1, std::min(opt->lay.n_chunks, most));
-    cudaError_t e = launch_overlapped(opt->state_bits == 8 ? adamw_kernel<8> : adamw_kernel<32>, dim3(grid), dim3(kAdamThreads), 0, (cudaStream_t)stream,
-                                      opt->ws, opt->lay, r);
+    const auto kernel = opt->state_bits == 8 ? step_kernel<8>(opt->grad_dtype, opt->param_dtype) : step_kernel<32>(opt->grad_dtype, opt->param_dtype);
+    cudaError_t e = launch_overlapped(kernel, dim3(grid), dim3(kAdamThreads), 0, (cudaStream_t)stream, opt->ws, opt->lay, r);
     return e == cudaSuccess ? EQL_OK : EQL_ERR_CUDA;
 }
 

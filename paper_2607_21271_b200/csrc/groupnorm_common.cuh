@@ -11,6 +11,7 @@
 #include <type_traits>
 
 #include "eql_internal.h"
+#include "packed.cuh"
 #include "ptx_sm100.cuh"
 
 namespace eql {
@@ -79,25 +80,6 @@ cudaError_t dispatch_io(int dtype, F&& f) {
     if (dtype == EQL_BF16) return f(__nv_bfloat16{});
     return f(float{});
 }
-
-// Two floats as one operand: a packed operation takes one issue slot, of which these kernels run out before anything else but the memory.
-__device__ __forceinline__ float2 pair(float v) { return make_float2(v, v); }
-#define EQL_PACKED(name, op)                                                                                                     \
-    __device__ __forceinline__ float2 name(float2 a, float2 b) {                                                                 \
-        float2 d;                                                                                                                \
-        asm(op ".rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t&>(d)) : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b))); \
-        return d;                                                                                                                \
-    }
-EQL_PACKED(add2, "add")
-EQL_PACKED(mul2, "mul")
-#undef EQL_PACKED
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-    float2 d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(reinterpret_cast<uint64_t&>(d)) : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)),
-        "l"(reinterpret_cast<uint64_t&>(c)));
-    return d;
-}
-__device__ __forceinline__ float2 sub2(float2 a, float2 b) { return fma2(b, pair(-1.0f), a); }
 
 // A vector of 16 bytes as pairs of floats.
 template <typename IO> struct NormIo;
@@ -169,17 +151,6 @@ __device__ __forceinline__ Moments warp_merge(Moments v) {
     }
     return v;                 // lane 0's
 }
-__device__ __forceinline__ float exp2_fast(float v) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-    return r;
-}
-__device__ __forceinline__ float reciprocal(float v) {
-    float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-    return r;
-}
-
 // The running form (Welford 1962) for columns of 2 P values, row after row: a fourth operation an element, and unlike with sums behind a
 // fixed pivot it does not matter how far the first value lies from the rest.
 template <int P>
@@ -205,8 +176,6 @@ __device__ __forceinline__ int64_t positions_of(const int32_t* lengths, int64_t 
     return n < 0 ? 0 : n > S ? S : n;
 }
 
-__device__ __forceinline__ float2 exp2_fast(float2 v) { return make_float2(exp2_fast(v.x), exp2_fast(v.y)); }
-__device__ __forceinline__ float2 reciprocal(float2 v) { return make_float2(reciprocal(v.x), reciprocal(v.y)); }
 
 __device__ __forceinline__ float2 minus_abs(float2 v) { return make_float2(-fabsf(v.x), -fabsf(v.y)); }
 

@@ -414,3 +414,39 @@ def test_many_tensors_of_every_size():
             within(part["v"], v, ev)
     finally:
         o.close()
+
+
+@pytest.mark.gpu
+def test_tensors_of_different_types_and_none_with_elements():
+    """One optimiser over parameters and gradients of several types gives the bits of one for each; one over empty tensors only counts."""
+    kinds = [("fp32", "fp32", False), ("bf16", "fp32", True), ("fp16", "fp16", False), ("bf16", "bf16", True)]
+    parts = [Optimiser((5000, 33), d, g, 8, m, seed=20 + i) for i, (d, g, m) in enumerate(kinds)]
+    same = [Optimiser((5000, 33), d, g, 8, m, seed=20 + i) for i, (d, g, m) in enumerate(kinds)]
+    table = [t for o in same for t in o.table]
+    bytes_ = eq.eqlinear_adamw_workspace_bytes(table, 8)
+    workspace = torch.empty(bytes_, dtype=torch.uint8, device="cuda")
+    s = torch.cuda.current_stream().cuda_stream
+    h = eq.eqlinear_adamw(table, 8, workspace, bytes_, s)
+    try:
+        for _ in range(2):
+            eq.eqlinear_adamw_step(h, 1e-3, stream=s)
+            for o in parts:
+                eq.eqlinear_adamw_step(o.h, 1e-3, stream=s)
+        for a, b in zip(parts, same):
+            b.check_guards()
+            for x, y in zip(a.snapshot(), b.snapshot()):
+                assert all(torch.equal(x[k], y[k]) for k in x)
+    finally:
+        torch.cuda.synchronize()
+        eq.eqlinear_adamw_destroy(h)
+        for o in parts + same:
+            o.close()
+    o = Optimiser((0, 0), "fp32", "fp32", 32, False, seed=30)
+    try:
+        norm = torch.full((1,), 9.0, device="cuda")
+        eq.eqlinear_adamw_clip(o.h, 1.0, norm=norm, stream=o.stream)
+        eq.eqlinear_adamw_step(o.h, 1e-3, stream=o.stream)
+        o.check_guards()
+        assert float(norm) == 0.0 and eq.eqlinear_adamw_info(o.h, o.stream).step == 1
+    finally:
+        o.close()
