@@ -369,7 +369,7 @@ eql_status_t eqlinear_groupnorm_bwd(const eql_groupnorm_t* norm, const void* x, 
  * States take 32 bits (float) or 8.  In 8 bits every 256 consecutive elements of a tensor share one float scale for m and
  * one for v: m is held as e4m3 codes of m * (448 / max|m|) with scale max|m| / 448, v as e5m2 codes of v * (57344 / max v)
  * with scale max v / 57344, both rounded to nearest even; a v above zero never becomes code zero (the least code, 2^-16,
- * stands for it), so that a later step does not divide by nothing.  A block whose largest magnitude is below 2^-100 is held
+ * stands for it), so that a later step does not divide by nothing.  A v below 2^-126 counts as zero in the denominator.  A block whose largest magnitude is below 2^-100 is held
  * as zeros.  The step itself uses the states before they are rounded.  Zeroed codes and scales are valid initial states. */
 typedef struct eqlinear_adamw_s* eqlinear_adamw_t;   /* opaque host object */
 

@@ -3,8 +3,9 @@
 // Everything here moves memory: per element a step reads the gradient, the two states and the parameter (or its float master) and
 // writes all but the gradient, 30 bytes with float states (float gradient, 16-bit parameter with master) or 18 with 8-bit ones, for
 // about 20 operations.  The unit of work is a chunk of 2048 elements of one tensor: eight warps, each one block of 256 elements, eight
-// per lane, so that the block that shares a scale is a warp and its maximum five shuffles.  The table of tensors and the
-// tensor of every chunk lie in the workspace; a CTA takes a contiguous run of chunks, and so meets a new tensor only now and then.
+// per lane, so that the block that shares a scale is a warp and its maximum one reduction.  The table of tensors and the
+// tensor of every chunk lie in the workspace; a CTA takes a contiguous run of chunks, and first fetches the part of the table that
+// these need, so that its loads of data do not wait for one entry of the table after the other.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -27,6 +28,7 @@ constexpr int kAdamThreads = 256;
 constexpr int kChunk = kBlock * (kAdamThreads / 32);
 constexpr int kNormCtasPerSm = 4, kStepCtasPerSm = 3;      // resident together, by their registers
 constexpr int kNormUnroll = 4;              // chunks of gradients that a warp has on their way
+constexpr int kTable = 32;                  // tensors that a CTA looks up at a time
 constexpr int kMaxNormCtas = 1024;
 constexpr float kE4m3Max = 448.0f, kE5m2Max = 57344.0f, kE5m2Least = 0x1p-16f, kTiny = 0x1p-100f;
 
@@ -38,7 +40,7 @@ struct Tensor {
     void *m, *v;
     float *m_scale, *v_scale;
     int64_t numel;
-    int32_t first_chunk;
+    int32_t first_chunk, chunks;
     int32_t param_dtype, grad_dtype;
     float weight_decay, lr_scale;
 };
@@ -137,6 +139,33 @@ __device__ __forceinline__ uint32_t encode4(const float2* q) {
 __device__ __forceinline__ float warp_max(float v) { return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v))); }
 __device__ __forceinline__ float& half_of(float2* v, int j) { return j % 2 ? v[j / 2].y : v[j / 2].x; }
 
+// A CTA's run of chunks, tensor by tensor: use(table, count, begin, end) for each part of the table in shared memory and its chunks.
+template <typename Use>
+__device__ __forceinline__ void for_chunks(char* ws, const Layout& lay, Tensor* table, Use&& use) {
+    const Tensor* tensors = reinterpret_cast<const Tensor*>(ws + lay.tensors);
+    const int32_t* chunk_tensor = reinterpret_cast<const int32_t*>(ws + lay.chunks);
+    const int begin = (int)(lay.n_chunks * blockIdx.x / gridDim.x), end = (int)(lay.n_chunks * (blockIdx.x + 1) / gridDim.x);
+    if (begin >= end) return;
+    const int last = chunk_tensor[end - 1];
+    int c = begin;
+    for (int first = chunk_tensor[begin]; first <= last; first += kTable) {
+        const int count = min(kTable, last + 1 - first);
+        __syncthreads();
+        static_assert(sizeof(Tensor) % 8 == 0, "copied in pieces of eight bytes");
+        for (int i = threadIdx.x; i < count * (int)(sizeof(Tensor) / 8); i += kAdamThreads)
+            reinterpret_cast<uint64_t*>(table)[i] = reinterpret_cast<const uint64_t*>(tensors + first)[i];
+        __syncthreads();
+        const int stop = min(end, table[count - 1].first_chunk + table[count - 1].chunks);
+        use(count, c, stop);
+        c = stop;
+    }
+}
+// The tensor of chunk c, from that of an earlier one on.
+__device__ __forceinline__ int tensor_of(const Tensor* table, int from, int c) {
+    while (c >= table[from].first_chunk + table[from].chunks) ++from;
+    return from;
+}
+
 // The step, states of BITS bits.  The moments are computed by separately rounded operations: in 8 bits, what lies next to the border
 // of two codes goes by their last bit, and a plain program has to come to the same codes.  (The assembler makes one fused operation of
 // a packed product and a packed sum, their rounding modes notwithstanding; a sum written as a * 1 + b, with a 1 that it does not
@@ -148,8 +177,7 @@ template <int BITS, int GRAD, int PARAM>
 __global__ void __launch_bounds__(kAdamThreads, kStepCtasPerSm) adamw_kernel(char* ws, Layout lay, Rates r) {
     ptx::grid_handover();
     Control* control = reinterpret_cast<Control*>(ws);
-    const Tensor* tensors = reinterpret_cast<const Tensor*>(ws + lay.tensors);
-    const int32_t* chunk_tensor = reinterpret_cast<const int32_t*>(ws + lay.chunks);
+    __shared__ Tensor table[kTable];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int32_t skip = control->skip;
     if (!skip) {
@@ -159,22 +187,15 @@ __global__ void __launch_bounds__(kAdamThreads, kStepCtasPerSm) adamw_kernel(cha
         const float correction1 = -expm1f((float)(t * r.log_beta1)), correction2 = -expm1f((float)(t * r.log_beta2));
         const float2 root2 = pair(rsqrtf(correction2)), eps = pair(r.eps);
         const float2 beta1 = pair(r.beta1), new1 = pair(r.one_minus_beta1), beta2 = pair(r.beta2), new2 = pair(r.one_minus_beta2), one = pair(r.one);
-        const int64_t begin = lay.n_chunks * blockIdx.x / gridDim.x, end = lay.n_chunks * (blockIdx.x + 1) / gridDim.x;
-        int32_t which = -1, next = begin < end ? chunk_tensor[begin] : 0;
-        Tensor x{};
-        float2 keep{}, size{};
-        for (int64_t c = begin; c < end; ++c) {
-            const int32_t now = next;
-            if (c + 1 < end) next = chunk_tensor[c + 1];
-            if (now != which) {
-                x = tensors[now];
-                which = now;
-                const float rate = lr * x.lr_scale;
-                keep = pair(1.0f - rate * x.weight_decay);
-                size = pair(-rate / correction1);
-            }
+        for_chunks(ws, lay, table, [&](int, int begin, int end) {
+          int which = 0;
+          for (int c = begin; c < end; ++c) {
+            which = tensor_of(table, which, c);
+            const Tensor& x = table[which];
+            const float rate = lr * x.lr_scale;
+            const float2 keep = pair(1.0f - rate * x.weight_decay), size = pair(__fdividef(-rate, correction1));
             const int grad_dtype = GRAD == kMixed ? x.grad_dtype : GRAD, param_dtype = PARAM == kMixed ? x.param_dtype : PARAM;
-            const int64_t base = (c - x.first_chunk) * kChunk + warp * kBlock;
+            const int64_t base = (int64_t)(c - x.first_chunk) * kChunk + warp * kBlock;
             const int64_t left = x.numel - base;
             if (left <= 0) continue;
             const bool full = left >= kBlock;
@@ -239,8 +260,8 @@ __global__ void __launch_bounds__(kAdamThreads, kStepCtasPerSm) adamw_kernel(cha
                     most_v = fmaxf(most_v, fmaxf(v[j].x, v[j].y));
                 }
                 float2 root;
-                asm("sqrt.approx.f32 %0, %1;" : "=f"(root.x) : "f"(v[j].x));
-                asm("sqrt.approx.f32 %0, %1;" : "=f"(root.y) : "f"(v[j].y));
+                asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(root.x) : "f"(v[j].x));
+                asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(root.y) : "f"(v[j].y));
                 p[j] = fma2(mul2(size, m[j]), reciprocal(fma2(root, root2, eps)), mul2(p[j], keep));
             }
             float2 qm[4], qv[4];
@@ -253,13 +274,19 @@ __global__ void __launch_bounds__(kAdamThreads, kStepCtasPerSm) adamw_kernel(cha
                 const float most = of_v ? most_v : most_m, top = of_v ? kE5m2Max : kE4m3Max;
                 const float ratio = (of_v ? fine_v : fine_m) ? __fdiv_rn(scale ? most : top, scale ? top : most) : 0.0f;
                 const float2 im = pair(__shfl_sync(0xffffffffu, ratio, 0)), iv = pair(__shfl_sync(0xffffffffu, ratio, 1));
-                const float least = fine_v ? kE5m2Least : 0.0f;
+                float smallest = kE5m2Least;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     qm[j] = mul2(m[j], im);
                     qv[j] = mul2(v[j], iv);
-                    if (v[j].x > 0.0f) qv[j].x = fmaxf(qv[j].x, least);
-                    if (v[j].y > 0.0f) qv[j].y = fmaxf(qv[j].y, least);
+                    smallest = fminf(smallest, fminf(qv[j].x, qv[j].y));
+                }
+                if (smallest < kE5m2Least && fine_v) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if (v[j].x > 0.0f) qv[j].x = fmaxf(qv[j].x, kE5m2Least);
+                        if (v[j].y > 0.0f) qv[j].y = fmaxf(qv[j].y, kE5m2Least);
+                    }
                 }
                 if (lane == 2) x.m_scale[block] = ratio;
                 if (lane == 3) x.v_scale[block] = ratio;
@@ -294,7 +321,8 @@ __global__ void __launch_bounds__(kAdamThreads, kStepCtasPerSm) adamw_kernel(cha
                     }
                 }
             }
-        }
+          }
+        });
     }
     // The last CTA to come here, when every CTA has read the control block, turns it to the next step.
     __syncthreads();
@@ -327,59 +355,50 @@ __device__ __forceinline__ double cta_sum(double v, double* shared) {
 __global__ void __launch_bounds__(kAdamThreads) grad_norm_kernel(char* ws, Layout lay, float max_norm, const float* loss_scale, float* norm_out) {
     ptx::grid_handover();
     Control* control = reinterpret_cast<Control*>(ws);
-    const Tensor* tensors = reinterpret_cast<const Tensor*>(ws + lay.tensors);
-    const int32_t* chunk_tensor = reinterpret_cast<const int32_t*>(ws + lay.chunks);
     double* partials = reinterpret_cast<double*>(ws + lay.partials);
+    __shared__ Tensor table[kTable];
     __shared__ double shared[kAdamThreads / 32];
     __shared__ bool last;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t begin = lay.n_chunks * blockIdx.x / gridDim.x, end = lay.n_chunks * (blockIdx.x + 1) / gridDim.x;
     double sums[4] = {};
-    auto add = [&](const uint4& u, int dtype) {
-        float2 f[2];
-        widen4(u, dtype, f);
-        sums[0] = fma((double)f[0].x, (double)f[0].x, sums[0]);
-        sums[1] = fma((double)f[0].y, (double)f[0].y, sums[1]);
-        sums[2] = fma((double)f[1].x, (double)f[1].x, sums[2]);
-        sums[3] = fma((double)f[1].y, (double)f[1].y, sums[3]);
-    };
-    int64_t c = begin;
-    while (c < end) {
-        const int32_t which = chunk_tensor[c];
-        const void* grad = tensors[which].grad;
-        const int64_t numel = tensors[which].numel;
-        const int dtype = tensors[which].grad_dtype;
-        // this tensor's chunks, several whole ones at a time
-        int64_t base = (c - tensors[which].first_chunk) * kChunk + warp * kBlock;
-        const int64_t mine = min(end - c, (numel - base + warp * kBlock + kChunk - 1) / kChunk);
-        int64_t k = 0;
-        for (; k + kNormUnroll <= mine && base + (kNormUnroll - 1) * kChunk + kBlock <= numel; k += kNormUnroll, base += kNormUnroll * kChunk) {
+    for_chunks(ws, lay, table, [&](int, int begin, int end) {
+        int which = 0;
+        for (int c = begin; c < end; c += kNormUnroll) {
             uint4 u[kNormUnroll][2];
+            int dtype[kNormUnroll];
 #pragma unroll
-            for (int i = 0; i < kNormUnroll; ++i)
+            for (int i = 0; i < kNormUnroll; ++i) {
+                dtype[i] = EQL_FP32;
+                u[i][0] = u[i][1] = make_uint4(0u, 0u, 0u, 0u);
+                if (c + i >= end) continue;
+                which = tensor_of(table, which, c + i);
+                const Tensor& x = table[which];
+                const int64_t base = (int64_t)(c + i - x.first_chunk) * kChunk + warp * kBlock;
+                if (x.numel - base >= kBlock) {
+                    dtype[i] = x.grad_dtype;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) u[i][h] = load_raw4(grad, base + i * kChunk + h * 128 + lane * 4, dtype);
+                    for (int h = 0; h < 2; ++h) u[i][h] = load_raw4(x.grad, base + h * 128 + lane * 4, x.grad_dtype);
+                } else {                                      // a tensor's end: what there is, as floats
 #pragma unroll
-            for (int i = 0; i < kNormUnroll; ++i)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) add(u[i][h], dtype);
-        }
-        for (; k < mine; ++k, base += kChunk) {
-            if (numel - base >= kBlock) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) add(load_raw4(grad, base + h * 128 + lane * 4, dtype), dtype);
-            } else {
-                for (int j = 0; j < 8; ++j) {
-                    const int64_t at = base + lane_element(lane, j);
-                    if (at < numel) {
-                        const double f = load_one(grad, at, dtype);
-                        sums[0] = fma(f, f, sums[0]);
+                    for (int j = 0; j < 8; ++j) {
+                        const int64_t at = base + lane_element(lane, j);
+                        if (at < x.numel) (&u[i][j >> 2].x)[j & 3] = __float_as_uint(load_one(x.grad, at, x.grad_dtype));
                     }
                 }
             }
+#pragma unroll
+            for (int i = 0; i < kNormUnroll; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float2 f[2];
+                    widen4(u[i][h], dtype[i], f);
+                    sums[0] = fma((double)f[0].x, (double)f[0].x, sums[0]);
+                    sums[1] = fma((double)f[0].y, (double)f[0].y, sums[1]);
+                    sums[2] = fma((double)f[1].x, (double)f[1].x, sums[2]);
+                    sums[3] = fma((double)f[1].y, (double)f[1].y, sums[3]);
+                }
         }
-        c += mine;
-    }
+    });
     double sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
     sum = cta_sum(sum, shared);
     if (threadIdx.x == 0) {
@@ -558,7 +577,7 @@ eql_status_t eqlinear_adamw(eqlinear_adamw_t* opt, const eql_adamw_tensor_t* ten
     for (int i = 0; i < count; ++i) {
         const eql_adamw_tensor_t& t = tensors[i];
         table[i] = Tensor{t.param, (float*)t.master, t.grad, t.exp_avg, t.exp_avg_sq, t.exp_avg_scale, t.exp_avg_sq_scale, t.numel, (int32_t)chunk,
-                          t.param_dtype, t.grad_dtype, t.weight_decay, t.lr_scale};
+                          (int32_t)chunks_of(t.numel), t.param_dtype, t.grad_dtype, t.weight_decay, t.lr_scale};
         for (int64_t k = chunks_of(t.numel); k > 0; --k) chunk_tensor[chunk++] = i;
     }
     cudaError_t e = cudaMemcpyAsync(workspace, image, lay.total, cudaMemcpyHostToDevice, s);
