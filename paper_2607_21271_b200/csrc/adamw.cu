@@ -27,7 +27,7 @@ constexpr int kBlock = 256;                 // elements that share a scale: one 
 constexpr int kAdamThreads = 256;
 constexpr int kChunk = kBlock * (kAdamThreads / 32);
 constexpr int kNormCtasPerSm = 4, kStepCtasPerSm = 3;      // resident together, by their registers
-constexpr int kNormUnroll = 4;              // chunks of gradients that a warp has on their way
+constexpr int kNormUnroll = 2;              // chunks of gradients that a warp has on their way
 constexpr int kTable = 32;                  // tensors that a CTA looks up at a time
 constexpr int kMaxNormCtas = 1024;
 constexpr float kE4m3Max = 448.0f, kE5m2Max = 57344.0f, kE5m2Least = 0x1p-16f, kTiny = 0x1p-100f;
@@ -67,17 +67,35 @@ struct Rates {
     const float* lr_device;
 };
 
-// Eight elements of a lane: two runs of four, 128 elements apart, so that a warp's access is one run of 128 elements.
-__device__ __forceinline__ int lane_element(int lane, int j) { return (j >> 2) * 128 + lane * 4 + (j & 3); }
+// A lane's eight elements are two runs of four, 128 elements apart, so that a warp's access is one run of 128 elements.
+constexpr int kRun = 128;
+// A block's elements, of which its tensor has `left` from its first on.
+__device__ __forceinline__ int block_elements(int64_t left) { return left >= kBlock ? kBlock : left > 0 ? (int)left : 0; }
 
-// Four elements as they lie in memory (16 bytes of float, 8 of a 16-bit type), fetched before any of them is looked at.
-__device__ __forceinline__ uint4 load_raw4(const void* base, int64_t at, int dtype) {
-    if (dtype == EQL_FP32) return __ldcs(reinterpret_cast<const uint4*>(static_cast<const float*>(base) + at));
-    const uint2 u = __ldcs(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(base) + at));
-    return make_uint4(u.x, u.y, 0u, 0u);
+// Four neighbouring elements as they lie in memory (SIZE bytes each, in the first words), fetched before any of them is looked at: from
+// `first` on in a block of `left`, at `at` in the tensor.  Those that a block at a tensor's end has not got count as zero.
+template <int SIZE>
+__device__ __forceinline__ uint4 load_raw4(const void* base, int64_t at, int first, int left) {
+    const char* from = static_cast<const char*>(base) + at * SIZE;
+    uint4 u = make_uint4(0u, 0u, 0u, 0u);
+    if (left >= kBlock) {                                     // a whole block: the same for all lanes
+        if (SIZE == 4) return __ldcs(reinterpret_cast<const uint4*>(from));
+        if (SIZE == 2) { const uint2 w = __ldcs(reinterpret_cast<const uint2*>(from)); u.x = w.x; u.y = w.y; }
+        if (SIZE == 1) u.x = __ldcs(reinterpret_cast<const uint32_t*>(from));
+        return u;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (first + j >= left) break;
+        uint32_t* word = &u.x + j * SIZE / 4;
+        if (SIZE == 4) *word = reinterpret_cast<const uint32_t*>(from)[j];
+        if (SIZE == 2) *word |= (uint32_t)reinterpret_cast<const uint16_t*>(from)[j] << (16 * (j & 1));
+        if (SIZE == 1) *word |= (uint32_t)reinterpret_cast<const uint8_t*>(from)[j] << (8 * j);
+    }
+    return u;
 }
-__device__ __forceinline__ float widen16(uint32_t bits, int dtype) {
-    return dtype == EQL_FP16 ? __half2float(__ushort_as_half((unsigned short)bits)) : __uint_as_float(bits << 16);
+__device__ __forceinline__ uint4 load_typed4(const void* base, int64_t at, int first, int left, int dtype) {
+    return dtype == EQL_FP32 ? load_raw4<4>(base, at, first, left) : load_raw4<2>(base, at, first, left);
 }
 __device__ __forceinline__ float2 widen_pair(uint32_t u, int dtype) {
     if (dtype == EQL_FP16) return __half22float2(*reinterpret_cast<const __half2*>(&u));
@@ -92,13 +110,6 @@ __device__ __forceinline__ void widen4(const uint4& u, int dtype, float2* f) {
         f[1] = widen_pair(u.y, dtype);
     }
 }
-__device__ __forceinline__ float load_one(const void* base, int64_t at, int dtype) {
-    if (dtype == EQL_FP32) return static_cast<const float*>(base)[at];
-    return widen16(static_cast<const uint16_t*>(base)[at], dtype);
-}
-__device__ __forceinline__ uint32_t narrow16(float v, int dtype) {
-    return dtype == EQL_FP16 ? __half_as_ushort(__float2half_rn(v)) : __bfloat16_as_ushort(__float2bfloat16_rn(v));
-}
 __device__ __forceinline__ uint32_t narrow_pair(float2 f, int dtype) {
     if (dtype == EQL_FP16) {
         const __half2 h = __floats2half2_rn(f.x, f.y);
@@ -107,15 +118,29 @@ __device__ __forceinline__ uint32_t narrow_pair(float2 f, int dtype) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(f.x, f.y);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
-__device__ __forceinline__ void store4(void* base, int64_t at, int dtype, const float2* f) {
-    if (dtype == EQL_FP32)
-        __stcs(reinterpret_cast<float4*>(static_cast<float*>(base) + at), make_float4(f[0].x, f[0].y, f[1].x, f[1].y));
-    else
-        __stcs(reinterpret_cast<uint2*>(static_cast<uint16_t*>(base) + at), make_uint2(narrow_pair(f[0], dtype), narrow_pair(f[1], dtype)));
+template <int SIZE>
+__device__ __forceinline__ void store_raw4(void* base, int64_t at, int first, int left, const uint4& u) {
+    char* to = static_cast<char*>(base) + at * SIZE;
+    if (left >= kBlock) {
+        if (SIZE == 4) __stcs(reinterpret_cast<uint4*>(to), u);
+        if (SIZE == 2) __stcs(reinterpret_cast<uint2*>(to), make_uint2(u.x, u.y));
+        if (SIZE == 1) __stcs(reinterpret_cast<uint32_t*>(to), u.x);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (first + j >= left) break;
+        const uint32_t word = *(&u.x + j * SIZE / 4);
+        if (SIZE == 4) reinterpret_cast<uint32_t*>(to)[j] = word;
+        if (SIZE == 2) reinterpret_cast<uint16_t*>(to)[j] = (uint16_t)(word >> (16 * (j & 1)));
+        if (SIZE == 1) reinterpret_cast<uint8_t*>(to)[j] = (uint8_t)(word >> (8 * j));
+    }
 }
-__device__ __forceinline__ void store_one(void* base, int64_t at, int dtype, float f) {
-    if (dtype == EQL_FP32) static_cast<float*>(base)[at] = f;
-    else static_cast<uint16_t*>(base)[at] = (uint16_t)narrow16(f, dtype);
+__device__ __forceinline__ void store_typed4(void* base, int64_t at, int first, int left, int dtype, const float2* f) {
+    if (dtype == EQL_FP32)
+        store_raw4<4>(base, at, first, left, make_uint4(__float_as_uint(f[0].x), __float_as_uint(f[0].y), __float_as_uint(f[1].x), __float_as_uint(f[1].y)));
+    else
+        store_raw4<2>(base, at, first, left, make_uint4(narrow_pair(f[0], dtype), narrow_pair(f[1], dtype), 0u, 0u));
 }
 
 template <__nv_fp8_interpretation_t KIND>
@@ -137,9 +162,8 @@ __device__ __forceinline__ uint32_t encode4(const float2* q) {
 
 // The largest of a warp's values, which are not negative: their bits are in the order of the values, NaN last.
 __device__ __forceinline__ float warp_max(float v) { return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v))); }
-__device__ __forceinline__ float& half_of(float2* v, int j) { return j % 2 ? v[j / 2].y : v[j / 2].x; }
 
-// A CTA's run of chunks, tensor by tensor: use(table, count, begin, end) for each part of the table in shared memory and its chunks.
+// A CTA's run of chunks, tensor by tensor: use(begin, end) for each part of the table in shared memory and its chunks.
 template <typename Use>
 __device__ __forceinline__ void for_chunks(char* ws, const Layout& lay, Tensor* table, Use&& use) {
     const Tensor* tensors = reinterpret_cast<const Tensor*>(ws + lay.tensors);
@@ -156,7 +180,7 @@ __device__ __forceinline__ void for_chunks(char* ws, const Layout& lay, Tensor* 
             reinterpret_cast<uint64_t*>(table)[i] = reinterpret_cast<const uint64_t*>(tensors + first)[i];
         __syncthreads();
         const int stop = min(end, table[count - 1].first_chunk + table[count - 1].chunks);
-        use(count, c, stop);
+        use(c, stop);
         c = stop;
     }
 }
@@ -171,6 +195,12 @@ __device__ __forceinline__ int tensor_of(const Tensor* table, int from, int c) {
 // a packed product and a packed sum, their rounding modes notwithstanding; a sum written as a * 1 + b, with a 1 that it does not
 // know, is left alone.)  The denominator may be a few float
 // roundings off (approximate square root and division, about 2^-22): it moves the parameter by lr times that.
+template <int BITS>
+struct Fetched {              // a lane's part of a block
+    int64_t base;
+    uint4 g[2], p[2], m[2], v[2];
+    float m_scale, v_scale;
+};
 // GRAD, PARAM: the type that all tensors have there, or kMixed.
 constexpr int kMixed = -1;
 template <int BITS, int GRAD, int PARAM>
@@ -187,68 +217,56 @@ __global__ void __launch_bounds__(kAdamThreads, kStepCtasPerSm) adamw_kernel(cha
         const float correction1 = -expm1f((float)(t * r.log_beta1)), correction2 = -expm1f((float)(t * r.log_beta2));
         const float2 root2 = pair(rsqrtf(correction2)), eps = pair(r.eps);
         const float2 beta1 = pair(r.beta1), new1 = pair(r.one_minus_beta1), beta2 = pair(r.beta2), new2 = pair(r.one_minus_beta2), one = pair(r.one);
-        for_chunks(ws, lay, table, [&](int, int begin, int end) {
-          int which = 0;
-          for (int c = begin; c < end; ++c) {
-            which = tensor_of(table, which, c);
-            const Tensor& x = table[which];
-            const float rate = lr * x.lr_scale;
-            const float2 keep = pair(1.0f - rate * x.weight_decay), size = pair(__fdividef(-rate, correction1));
-            const int grad_dtype = GRAD == kMixed ? x.grad_dtype : GRAD, param_dtype = PARAM == kMixed ? x.param_dtype : PARAM;
-            const int64_t base = (int64_t)(c - x.first_chunk) * kChunk + warp * kBlock;
-            const int64_t left = x.numel - base;
-            if (left <= 0) continue;
-            const bool full = left >= kBlock;
-            float2 g[4], m[4], v[4], p[4];
-            const void* from = x.master ? (const void*)x.master : (const void*)x.param;
-            const int from_dtype = x.master ? (int)EQL_FP32 : param_dtype;
-            const int64_t block = base / kBlock;
-            float2 ms{}, vs{};
-            if (BITS == 8) { ms = pair(x.m_scale[block]); vs = pair(x.v_scale[block]); }
-            if (full) {
-                uint4 rg[2], rp[2], rm[2], rv[2];
+        for_chunks(ws, lay, table, [&](int begin, int end) {
+            // A block is fetched while the one before is computed: with 8-bit states, whose arithmetic takes as long as the memory does.
+            constexpr bool kAhead = BITS == 8;
+            Fetched<BITS> next;
+            int ahead = 0;
+            auto fetch = [&](int c) {
+                ahead = tensor_of(table, ahead, c);
+                const Tensor& x = table[ahead];
+                next.base = (int64_t)(c - x.first_chunk) * kChunk + warp * kBlock;
+                const int left = block_elements(x.numel - next.base);
+                if (left == 0) return;
+                if (BITS == 8) { next.m_scale = x.m_scale[next.base / kBlock]; next.v_scale = x.v_scale[next.base / kBlock]; }
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int64_t at = base + h * 128 + lane * 4;
-                    rg[h] = load_raw4(x.grad, at, grad_dtype);
-                    rp[h] = load_raw4(from, at, from_dtype);
-                    if (BITS == 32) {
-                        rm[h] = load_raw4(x.m, at, EQL_FP32);
-                        rv[h] = load_raw4(x.v, at, EQL_FP32);
-                    } else {
-                        rm[h].x = __ldcs(reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(x.m) + at));
-                        rv[h].x = __ldcs(reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(x.v) + at));
-                    }
+                    const int first = h * kRun + lane * 4;
+                    const int64_t at = next.base + first;
+                    next.g[h] = load_typed4(x.grad, at, first, left, GRAD == kMixed ? x.grad_dtype : GRAD);
+                    next.p[h] = x.master ? load_raw4<4>(x.master, at, first, left) : load_typed4(x.param, at, first, left, PARAM == kMixed ? x.param_dtype : PARAM);
+                    next.m[h] = load_raw4<BITS / 8>(x.m, at, first, left);
+                    next.v[h] = load_raw4<BITS / 8>(x.v, at, first, left);
                 }
+            };
+            int which = 0;
+            if (kAhead) fetch(begin);
+            for (int c = begin; c < end; ++c) {
+                if (!kAhead) fetch(c);
+                const Fetched<BITS> now = next;
+                which = kAhead ? tensor_of(table, which, c) : ahead;
+                if (kAhead && c + 1 < end) fetch(c + 1);
+                const Tensor& x = table[which];
+                const int left = block_elements(x.numel - now.base);
+                if (left == 0) continue;
+                const float rate = lr * x.lr_scale;
+                const float2 keep = pair(1.0f - rate * x.weight_decay), size = pair(__fdividef(-rate, correction1));
+                const int grad_dtype = GRAD == kMixed ? x.grad_dtype : GRAD, param_dtype = PARAM == kMixed ? x.param_dtype : PARAM;
+                const int64_t block = now.base / kBlock;
+                float2 g[4], m[4], v[4], p[4];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    widen4(rg[h], grad_dtype, g + 2 * h);
-                    widen4(rp[h], from_dtype, p + 2 * h);
+                    widen4(now.g[h], grad_dtype, g + 2 * h);
+                    if (x.master) widen4(now.p[h], EQL_FP32, p + 2 * h);
+                    else widen4(now.p[h], param_dtype, p + 2 * h);
                     if (BITS == 32) {
-                        widen4(rm[h], EQL_FP32, m + 2 * h);
-                        widen4(rv[h], EQL_FP32, v + 2 * h);
+                        widen4(now.m[h], EQL_FP32, m + 2 * h);
+                        widen4(now.v[h], EQL_FP32, v + 2 * h);
                     } else {
-                        decode4<__NV_E4M3>(rm[h].x, ms, m + 2 * h);
-                        decode4<__NV_E5M2>(rv[h].x, vs, v + 2 * h);
+                        decode4<__NV_E4M3>(now.m[h].x, pair(now.m_scale), m + 2 * h);
+                        decode4<__NV_E5M2>(now.v[h].x, pair(now.v_scale), v + 2 * h);
                     }
                 }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    half_of(g, j) = half_of(m, j) = half_of(v, j) = half_of(p, j) = 0.0f;
-                    const int64_t at = base + lane_element(lane, j);
-                    if (at >= x.numel) continue;
-                    half_of(g, j) = load_one(x.grad, at, grad_dtype);
-                    half_of(p, j) = load_one(from, at, from_dtype);
-                    if (BITS == 32) {
-                        half_of(m, j) = static_cast<const float*>(x.m)[at];
-                        half_of(v, j) = static_cast<const float*>(x.v)[at];
-                    } else {
-                        half_of(m, j) = decode_pair<__NV_E4M3>(static_cast<const uint8_t*>(x.m)[at], ms).x;
-                        half_of(v, j) = decode_pair<__NV_E5M2>(static_cast<const uint8_t*>(x.v)[at], vs).x;
-                    }
-                }
-            }
             float most_m = 0.0f, most_v = 0.0f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -291,37 +309,21 @@ __global__ void __launch_bounds__(kAdamThreads, kStepCtasPerSm) adamw_kernel(cha
                 if (lane == 2) x.m_scale[block] = ratio;
                 if (lane == 3) x.v_scale[block] = ratio;
             }
-            if (full) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int64_t at = base + h * 128 + lane * 4;
-                    if (x.master) store4(x.master, at, EQL_FP32, p + 2 * h);
-                    store4(x.param, at, param_dtype, p + 2 * h);
-                    if (BITS == 32) {
-                        store4(x.m, at, EQL_FP32, m + 2 * h);
-                        store4(x.v, at, EQL_FP32, v + 2 * h);
-                    } else {
-                        __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(x.m) + at), encode4<__NV_E4M3>(qm + 2 * h));
-                        __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(x.v) + at), encode4<__NV_E5M2>(qv + 2 * h));
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int64_t at = base + lane_element(lane, j);
-                    if (at >= x.numel) continue;
-                    if (x.master) x.master[at] = half_of(p, j);
-                    store_one(x.param, at, param_dtype, half_of(p, j));
-                    if (BITS == 32) {
-                        static_cast<float*>(x.m)[at] = half_of(m, j);
-                        static_cast<float*>(x.v)[at] = half_of(v, j);
-                    } else {
-                        static_cast<uint8_t*>(x.m)[at] = __nv_cvt_float_to_fp8(half_of(qm, j), __NV_SATFINITE, __NV_E4M3);
-                        static_cast<uint8_t*>(x.v)[at] = __nv_cvt_float_to_fp8(half_of(qv, j), __NV_SATFINITE, __NV_E5M2);
-                    }
+            for (int h = 0; h < 2; ++h) {
+                const int first = h * kRun + lane * 4;
+                const int64_t at = now.base + first;
+                if (x.master) store_typed4(x.master, at, first, left, EQL_FP32, p + 2 * h);
+                store_typed4(x.param, at, first, left, param_dtype, p + 2 * h);
+                if (BITS == 32) {
+                    store_typed4(x.m, at, first, left, EQL_FP32, m + 2 * h);
+                    store_typed4(x.v, at, first, left, EQL_FP32, v + 2 * h);
+                } else {
+                    store_raw4<1>(x.m, at, first, left, make_uint4(encode4<__NV_E4M3>(qm + 2 * h), 0u, 0u, 0u));
+                    store_raw4<1>(x.v, at, first, left, make_uint4(encode4<__NV_E5M2>(qv + 2 * h), 0u, 0u, 0u));
                 }
             }
-          }
+            }
         });
     }
     // The last CTA to come here, when every CTA has read the control block, turns it to the next step.
@@ -352,7 +354,8 @@ __device__ __forceinline__ double cta_sum(double v, double* shared) {
 // Sum of squares in double: a float's square is exact there and no sum overflows, so the total is finite exactly where every gradient
 // is, and its rounding to float does not depend on the order of the sum (but for one in 10^8).  The last CTA adds the CTAs' sums
 // in the order of their numbers.
-__global__ void __launch_bounds__(kAdamThreads) grad_norm_kernel(char* ws, Layout lay, float max_norm, const float* loss_scale, float* norm_out) {
+template <int GRAD>
+__global__ void __launch_bounds__(kAdamThreads, kNormCtasPerSm) grad_norm_kernel(char* ws, Layout lay, float max_norm, const float* loss_scale, float* norm_out) {
     ptx::grid_handover();
     Control* control = reinterpret_cast<Control*>(ws);
     double* partials = reinterpret_cast<double*>(ws + lay.partials);
@@ -361,30 +364,23 @@ __global__ void __launch_bounds__(kAdamThreads) grad_norm_kernel(char* ws, Layou
     __shared__ bool last;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     double sums[4] = {};
-    for_chunks(ws, lay, table, [&](int, int begin, int end) {
+    for_chunks(ws, lay, table, [&](int begin, int end) {
         int which = 0;
         for (int c = begin; c < end; c += kNormUnroll) {
             uint4 u[kNormUnroll][2];
             int dtype[kNormUnroll];
 #pragma unroll
             for (int i = 0; i < kNormUnroll; ++i) {
-                dtype[i] = EQL_FP32;
+                dtype[i] = GRAD == kMixed ? (int)EQL_FP32 : GRAD;
                 u[i][0] = u[i][1] = make_uint4(0u, 0u, 0u, 0u);
                 if (c + i >= end) continue;
                 which = tensor_of(table, which, c + i);
                 const Tensor& x = table[which];
+                if (GRAD == kMixed) dtype[i] = x.grad_dtype;
                 const int64_t base = (int64_t)(c + i - x.first_chunk) * kChunk + warp * kBlock;
-                if (x.numel - base >= kBlock) {
-                    dtype[i] = x.grad_dtype;
+                const int left = block_elements(x.numel - base);
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) u[i][h] = load_raw4(x.grad, base + h * 128 + lane * 4, x.grad_dtype);
-                } else {                                      // a tensor's end: what there is, as floats
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int64_t at = base + lane_element(lane, j);
-                        if (at < x.numel) (&u[i][j >> 2].x)[j & 3] = __float_as_uint(load_one(x.grad, at, x.grad_dtype));
-                    }
-                }
+                for (int h = 0; h < 2; ++h) u[i][h] = load_typed4(x.grad, base + h * kRun + lane * 4, h * kRun + lane * 4, left, dtype[i]);
             }
 #pragma unroll
             for (int i = 0; i < kNormUnroll; ++i)
@@ -600,7 +596,9 @@ eql_status_t eqlinear_adamw_clip(eqlinear_adamw_t opt, float max_norm, const flo
     if (!aligned(loss_scale, 4) || !aligned(norm, 4)) return EQL_ERR_ALIGNMENT;
     const int64_t most = std::min(opt->num_sms * kNormCtasPerSm, kMaxNormCtas);
     const unsigned grid = (unsigned)std::max<int64_t>(1, std::min(opt->lay.n_chunks, most));
-    cudaError_t e = launch_overlapped(grad_norm_kernel, dim3(grid), dim3(kAdamThreads), 0, (cudaStream_t)stream, opt->ws, opt->lay, max_norm,
+    const auto kernel = opt->grad_dtype == kMixed ? grad_norm_kernel<kMixed> : opt->grad_dtype == EQL_FP32 ? grad_norm_kernel<EQL_FP32>
+                        : opt->grad_dtype == EQL_FP16 ? grad_norm_kernel<EQL_FP16> : grad_norm_kernel<EQL_BF16>;
+    cudaError_t e = launch_overlapped(kernel, dim3(grid), dim3(kAdamThreads), 0, (cudaStream_t)stream, opt->ws, opt->lay, max_norm,
                                       loss_scale, norm);
     return e == cudaSuccess ? EQL_OK : EQL_ERR_CUDA;
 }
