@@ -4,8 +4,8 @@
 // writes all but the gradient, 30 bytes with float states (float gradient, 16-bit parameter with master) or 18 with 8-bit ones, for
 // about 20 operations.  The unit of work is a chunk of 2048 elements of one tensor: eight warps, each one block of 256 elements, eight
 // per lane, so that the block that shares a scale is a warp and its maximum one reduction.  The table of tensors and the
-// tensor of every chunk lie in the workspace; a CTA takes a contiguous run of chunks, and first fetches the part of the table that
-// these need, so that its loads of data do not wait for one entry of the table after the other.
+// tensor of every chunk lie in the workspace; a CTA looks up its next 32 chunks at once, so that its loads of data do not wait for one
+// entry of the table after the other.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -26,8 +26,11 @@ namespace {
 constexpr int kBlock = 256;                 // elements that share a scale: one warp's
 constexpr int kAdamThreads = 256;
 constexpr int kChunk = kBlock * (kAdamThreads / 32);
-constexpr int kNormCtasPerSm = 4, kStepCtasPerSm = 3;      // resident together, by their registers
-constexpr int kNormUnroll = 2;              // chunks of gradients that a warp has on their way
+// CTAs resident together, by their registers.  (With float states, 10.6 million weights and the norm: two 67 us, three 73, four 73; with
+// 8-bit ones, 134 million: two 478, three 467, four 473.)
+constexpr int kNormCtasPerSm = 4;
+constexpr int step_ctas_per_sm(int bits) { return bits == 8 ? 3 : 2; }
+constexpr int kNormUnroll = 4;              // chunks of gradients that a warp has on their way
 constexpr int kTable = 32;                  // tensors that a CTA looks up at a time
 constexpr int kMaxNormCtas = 1024;
 constexpr float kE4m3Max = 448.0f, kE5m2Max = 57344.0f, kE5m2Least = 0x1p-16f, kTiny = 0x1p-100f;
@@ -40,9 +43,10 @@ struct Tensor {
     void *m, *v;
     float *m_scale, *v_scale;
     int64_t numel;
-    int32_t first_chunk, chunks;
+    int32_t first_chunk;
     int32_t param_dtype, grad_dtype;
     float weight_decay, lr_scale;
+    int32_t unused;           // (whole pieces of eight bytes)
 };
 
 // The optimiser's own state, at the start of the workspace.
@@ -69,33 +73,44 @@ struct Rates {
 
 // A lane's eight elements are two runs of four, 128 elements apart, so that a warp's access is one run of 128 elements.
 constexpr int kRun = 128;
-// A block's elements, of which its tensor has `left` from its first on.
-__device__ __forceinline__ int block_elements(int64_t left) { return left >= kBlock ? kBlock : left > 0 ? (int)left : 0; }
 
-// Four neighbouring elements as they lie in memory (SIZE bytes each, in the first words), fetched before any of them is looked at: from
-// `first` on in a block of `left`, at `at` in the tensor.  Those that a block at a tensor's end has not got count as zero.
+// Four neighbouring elements as they lie in memory, SIZE bytes each, in the first words; fetched before any of them is looked at.
 template <int SIZE>
-__device__ __forceinline__ uint4 load_raw4(const void* base, int64_t at, int first, int left) {
-    const char* from = static_cast<const char*>(base) + at * SIZE;
+__device__ __forceinline__ uint4 load_raw4(const void* from) {
+    if (SIZE == 4) return __ldcs(static_cast<const uint4*>(from));
+    if (SIZE == 2) { const uint2 w = __ldcs(static_cast<const uint2*>(from)); return make_uint4(w.x, w.y, 0u, 0u); }
+    return make_uint4(__ldcs(static_cast<const uint32_t*>(from)), 0u, 0u, 0u);
+}
+template <int SIZE>
+__device__ __forceinline__ void store_raw4(void* to, const uint4& u) {
+    if (SIZE == 4) __stcs(static_cast<uint4*>(to), u);
+    if (SIZE == 2) __stcs(static_cast<uint2*>(to), make_uint2(u.x, u.y));
+    if (SIZE == 1) __stcs(static_cast<uint32_t*>(to), u.x);
+}
+// The same, as far as a tensor goes: `left` elements from there on, the others count as zero.
+template <int SIZE>
+__device__ __forceinline__ uint4 load_some4(const void* from, int left) {
     uint4 u = make_uint4(0u, 0u, 0u, 0u);
-    if (left >= kBlock) {                                     // a whole block: the same for all lanes
-        if (SIZE == 4) return __ldcs(reinterpret_cast<const uint4*>(from));
-        if (SIZE == 2) { const uint2 w = __ldcs(reinterpret_cast<const uint2*>(from)); u.x = w.x; u.y = w.y; }
-        if (SIZE == 1) u.x = __ldcs(reinterpret_cast<const uint32_t*>(from));
-        return u;
-    }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        if (first + j >= left) break;
-        uint32_t* word = &u.x + j * SIZE / 4;
-        if (SIZE == 4) *word = reinterpret_cast<const uint32_t*>(from)[j];
-        if (SIZE == 2) *word |= (uint32_t)reinterpret_cast<const uint16_t*>(from)[j] << (16 * (j & 1));
-        if (SIZE == 1) *word |= (uint32_t)reinterpret_cast<const uint8_t*>(from)[j] << (8 * j);
+        if (j >= left) break;
+        uint32_t& word = (&u.x)[j * SIZE / 4];
+        if (SIZE == 4) word = static_cast<const uint32_t*>(from)[j];
+        if (SIZE == 2) word |= (uint32_t)static_cast<const uint16_t*>(from)[j] << (16 * (j & 1));
+        if (SIZE == 1) word |= (uint32_t)static_cast<const uint8_t*>(from)[j] << (8 * j);
     }
     return u;
 }
-__device__ __forceinline__ uint4 load_typed4(const void* base, int64_t at, int first, int left, int dtype) {
-    return dtype == EQL_FP32 ? load_raw4<4>(base, at, first, left) : load_raw4<2>(base, at, first, left);
+template <int SIZE>
+__device__ __forceinline__ void store_some4(void* to, int left, const uint4& u) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (j >= left) break;
+        const uint32_t word = (&u.x)[j * SIZE / 4];
+        if (SIZE == 4) static_cast<uint32_t*>(to)[j] = word;
+        if (SIZE == 2) static_cast<uint16_t*>(to)[j] = (uint16_t)(word >> (16 * (j & 1)));
+        if (SIZE == 1) static_cast<uint8_t*>(to)[j] = (uint8_t)(word >> (8 * j));
+    }
 }
 __device__ __forceinline__ float2 widen_pair(uint32_t u, int dtype) {
     if (dtype == EQL_FP16) return __half22float2(*reinterpret_cast<const __half2*>(&u));
@@ -118,29 +133,9 @@ __device__ __forceinline__ uint32_t narrow_pair(float2 f, int dtype) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(f.x, f.y);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
-template <int SIZE>
-__device__ __forceinline__ void store_raw4(void* base, int64_t at, int first, int left, const uint4& u) {
-    char* to = static_cast<char*>(base) + at * SIZE;
-    if (left >= kBlock) {
-        if (SIZE == 4) __stcs(reinterpret_cast<uint4*>(to), u);
-        if (SIZE == 2) __stcs(reinterpret_cast<uint2*>(to), make_uint2(u.x, u.y));
-        if (SIZE == 1) __stcs(reinterpret_cast<uint32_t*>(to), u.x);
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if (first + j >= left) break;
-        const uint32_t word = *(&u.x + j * SIZE / 4);
-        if (SIZE == 4) reinterpret_cast<uint32_t*>(to)[j] = word;
-        if (SIZE == 2) reinterpret_cast<uint16_t*>(to)[j] = (uint16_t)(word >> (16 * (j & 1)));
-        if (SIZE == 1) reinterpret_cast<uint8_t*>(to)[j] = (uint8_t)(word >> (8 * j));
-    }
-}
-__device__ __forceinline__ void store_typed4(void* base, int64_t at, int first, int left, int dtype, const float2* f) {
-    if (dtype == EQL_FP32)
-        store_raw4<4>(base, at, first, left, make_uint4(__float_as_uint(f[0].x), __float_as_uint(f[0].y), __float_as_uint(f[1].x), __float_as_uint(f[1].y)));
-    else
-        store_raw4<2>(base, at, first, left, make_uint4(narrow_pair(f[0], dtype), narrow_pair(f[1], dtype), 0u, 0u));
+__device__ __forceinline__ uint4 narrow4(const float2* f, int dtype) {
+    if (dtype == EQL_FP32) return make_uint4(__float_as_uint(f[0].x), __float_as_uint(f[0].y), __float_as_uint(f[1].x), __float_as_uint(f[1].y));
+    return make_uint4(narrow_pair(f[0], dtype), narrow_pair(f[1], dtype), 0u, 0u);
 }
 
 template <__nv_fp8_interpretation_t KIND>
@@ -163,166 +158,235 @@ __device__ __forceinline__ uint32_t encode4(const float2* q) {
 // The largest of a warp's values, which are not negative: their bits are in the order of the values, NaN last.
 __device__ __forceinline__ float warp_max(float v) { return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v))); }
 
-// A CTA's run of chunks, tensor by tensor: use(begin, end) for each part of the table in shared memory and its chunks.
+// A CTA's chunks: all CTAs together sweep over the tensors, so that what is under way at a time lies close together in memory (with a
+// contiguous run of chunks for each CTA, 134 million weights took 462 us instead of 389).  The tensors of the next chunks are looked up
+// for all of them at once: use(table, first, count), entry i of the table being that of chunk first + i * gridDim.x.
 template <typename Use>
 __device__ __forceinline__ void for_chunks(char* ws, const Layout& lay, Tensor* table, Use&& use) {
-    const Tensor* tensors = reinterpret_cast<const Tensor*>(ws + lay.tensors);
+    constexpr int kPieces = sizeof(Tensor) / 8;
+    static_assert(sizeof(Tensor) % 8 == 0, "copied in pieces of eight bytes");
+    const uint64_t* tensors = reinterpret_cast<const uint64_t*>(ws + lay.tensors);
     const int32_t* chunk_tensor = reinterpret_cast<const int32_t*>(ws + lay.chunks);
-    const int begin = (int)(lay.n_chunks * blockIdx.x / gridDim.x), end = (int)(lay.n_chunks * (blockIdx.x + 1) / gridDim.x);
-    if (begin >= end) return;
-    const int last = chunk_tensor[end - 1];
-    int c = begin;
-    for (int first = chunk_tensor[begin]; first <= last; first += kTable) {
-        const int count = min(kTable, last + 1 - first);
+    for (int64_t first = blockIdx.x; first < lay.n_chunks; first += (int64_t)kTable * gridDim.x) {
+        const int64_t left = (lay.n_chunks - first + gridDim.x - 1) / gridDim.x;
+        const int count = left < kTable ? (int)left : kTable;
         __syncthreads();
-        static_assert(sizeof(Tensor) % 8 == 0, "copied in pieces of eight bytes");
-        for (int i = threadIdx.x; i < count * (int)(sizeof(Tensor) / 8); i += kAdamThreads)
-            reinterpret_cast<uint64_t*>(table)[i] = reinterpret_cast<const uint64_t*>(tensors + first)[i];
+        for (int i = threadIdx.x; i < count * kPieces; i += kAdamThreads) {
+            const int entry = i / kPieces, piece = i - entry * kPieces;
+            reinterpret_cast<uint64_t*>(table + entry)[piece] = tensors[(int64_t)chunk_tensor[first + (int64_t)entry * gridDim.x] * kPieces + piece];
+        }
         __syncthreads();
-        const int stop = min(end, table[count - 1].first_chunk + table[count - 1].chunks);
-        use(c, stop);
-        c = stop;
+        use(first, count);
     }
 }
-// The tensor of chunk c, from that of an earlier one on.
-__device__ __forceinline__ int tensor_of(const Tensor* table, int from, int c) {
-    while (c >= table[from].first_chunk + table[from].chunks) ++from;
-    return from;
-}
-
-// The step, states of BITS bits.  The moments are computed by separately rounded operations: in 8 bits, what lies next to the border
-// of two codes goes by their last bit, and a plain program has to come to the same codes.  (The assembler makes one fused operation of
-// a packed product and a packed sum, their rounding modes notwithstanding; a sum written as a * 1 + b, with a 1 that it does not
-// know, is left alone.)  The denominator may be a few float
-// roundings off (approximate square root and division, about 2^-22): it moves the parameter by lr times that.
-template <int BITS>
-struct Fetched {              // a lane's part of a block
+// The warp's block in chunk c: its first element, and how many its tensor has from there on (as far as a block goes).
+struct Block {
     int64_t base;
+    int count;
+    __device__ __forceinline__ Block(const Tensor& x, int64_t c) : base((c - x.first_chunk) * kChunk + (threadIdx.x >> 5) * kBlock) {
+        const int64_t left = x.numel - base;
+        count = left >= kBlock ? kBlock : left > 0 ? (int)left : 0;
+    }
+};
+
+// A lane's part of a block, as it lies in memory.
+template <int BITS>
+struct Fetched {
     uint4 g[2], p[2], m[2], v[2];
     float m_scale, v_scale;
 };
+// The same for the packed operations.
+struct Formula {
+    float2 factor, beta1, new1, beta2, new2, one, eps, root2;
+};
+
+// One block.  The moments are computed by separately rounded operations: in 8 bits, what lies next to the border of two codes goes by
+// their last bit, and a plain program has to come to the same codes.  (The assembler makes one fused operation of a packed product
+// and a packed sum, their rounding modes notwithstanding; a sum written as a * 1 + b, with a 1 that it does not know, is left alone.)
+// The denominator may be a few float roundings off (approximate square root and reciprocal, about 2^-22): it moves the parameter by lr
+// times that.
+template <int BITS>
+__device__ __forceinline__ void update(const Formula& f, Fetched<BITS>& b, int grad_dtype, int from_dtype, float2 keep, float2 size, float2* p) {
+    float2 g[4], m[4], v[4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        widen4(b.g[h], grad_dtype, g + 2 * h);
+        widen4(b.p[h], from_dtype, p + 2 * h);
+        if (BITS == 32) {
+            widen4(b.m[h], EQL_FP32, m + 2 * h);
+            widen4(b.v[h], EQL_FP32, v + 2 * h);
+        } else {
+            decode4<__NV_E4M3>(b.m[h].x, pair(b.m_scale), m + 2 * h);
+            decode4<__NV_E5M2>(b.v[h].x, pair(b.v_scale), v + 2 * h);
+        }
+    }
+    float most_m = 0.0f, most_v = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float2 gs = mul2(g[j], f.factor);
+        m[j] = fma2(mul2(m[j], f.beta1), f.one, mul2(gs, f.new1));
+        v[j] = fma2(mul2(v[j], f.beta2), f.one, mul2(mul2(gs, gs), f.new2));
+        if (BITS == 8) {
+            most_m = fmaxf(most_m, fmaxf(fabsf(m[j].x), fabsf(m[j].y)));
+            most_v = fmaxf(most_v, fmaxf(v[j].x, v[j].y));
+        }
+        float2 root;
+        asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(root.x) : "f"(v[j].x));
+        asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(root.y) : "f"(v[j].y));
+        p[j] = fma2(mul2(size, m[j]), reciprocal(fma2(root, f.root2, f.eps)), mul2(p[j], keep));
+    }
+    if (BITS == 32) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            b.m[h] = narrow4(m + 2 * h, EQL_FP32);
+            b.v[h] = narrow4(v + 2 * h, EQL_FP32);
+        }
+        return;
+    }
+    most_m = warp_max(most_m);
+    most_v = warp_max(most_v);
+    const bool fine_m = !(most_m < kTiny), fine_v = !(most_v < kTiny);
+    // the block's four divisions, each in another lane: the inverse scales of m and v, and the scales
+    const int lane = threadIdx.x & 31;
+    const bool of_v = lane & 1, scale = lane & 2;
+    const float most = of_v ? most_v : most_m, top = of_v ? kE5m2Max : kE4m3Max;
+    const float ratio = (of_v ? fine_v : fine_m) ? __fdiv_rn(scale ? most : top, scale ? top : most) : 0.0f;
+    const float2 im = pair(__shfl_sync(0xffffffffu, ratio, 0)), iv = pair(__shfl_sync(0xffffffffu, ratio, 1));
+    float smallest = kE5m2Least;
+    float2 qm[4], qv[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        qm[j] = mul2(m[j], im);
+        qv[j] = mul2(v[j], iv);
+        smallest = fminf(smallest, fminf(qv[j].x, qv[j].y));
+    }
+    if (smallest < kE5m2Least && fine_v) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (v[j].x > 0.0f) qv[j].x = fmaxf(qv[j].x, kE5m2Least);
+            if (v[j].y > 0.0f) qv[j].y = fmaxf(qv[j].y, kE5m2Least);
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        b.m[h].x = encode4<__NV_E4M3>(qm + 2 * h);
+        b.v[h].x = encode4<__NV_E5M2>(qv + 2 * h);
+    }
+    b.m_scale = b.v_scale = ratio;                            // lane 2's and lane 3's
+}
+
+// A block at a tensor's end.
+template <int BITS>
+__device__ __noinline__ void update_end(const Formula& f, const Tensor& x, int64_t base, int count, float2 keep, float2 size) {
+    constexpr int S = BITS / 8;
+    const int lane = threadIdx.x & 31;
+    const int64_t block = base / kBlock;
+    Fetched<BITS> b;
+    float2 p[4];
+    if (BITS == 8) { b.m_scale = x.m_scale[block]; b.v_scale = x.v_scale[block]; }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int64_t at = base + h * kRun + lane * 4;
+        const int left = count - h * kRun - lane * 4;
+        b.g[h] = x.grad_dtype == EQL_FP32 ? load_some4<4>((const float*)x.grad + at, left) : load_some4<2>((const uint16_t*)x.grad + at, left);
+        b.p[h] = x.master ? load_some4<4>(x.master + at, left) : x.param_dtype == EQL_FP32 ? load_some4<4>((const float*)x.param + at, left)
+                                                                                          : load_some4<2>((const uint16_t*)x.param + at, left);
+        b.m[h] = load_some4<S>((const char*)x.m + at * S, left);
+        b.v[h] = load_some4<S>((const char*)x.v + at * S, left);
+    }
+    update<BITS>(f, b, x.grad_dtype, x.master ? (int)EQL_FP32 : x.param_dtype, keep, size, p);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int64_t at = base + h * kRun + lane * 4;
+        const int left = count - h * kRun - lane * 4;
+        if (x.master) store_some4<4>(x.master + at, left, narrow4(p + 2 * h, EQL_FP32));
+        if (x.param_dtype == EQL_FP32) store_some4<4>((float*)x.param + at, left, narrow4(p + 2 * h, EQL_FP32));
+        else store_some4<2>((uint16_t*)x.param + at, left, narrow4(p + 2 * h, x.param_dtype));
+        store_some4<S>((char*)x.m + at * S, left, b.m[h]);
+        store_some4<S>((char*)x.v + at * S, left, b.v[h]);
+    }
+    if (BITS == 8 && lane == 2) x.m_scale[block] = b.m_scale;
+    if (BITS == 8 && lane == 3) x.v_scale[block] = b.v_scale;
+}
+
 // GRAD, PARAM: the type that all tensors have there, or kMixed.
 constexpr int kMixed = -1;
 template <int BITS, int GRAD, int PARAM>
-__global__ void __launch_bounds__(kAdamThreads, kStepCtasPerSm) adamw_kernel(char* ws, Layout lay, Rates r) {
+__global__ void __launch_bounds__(kAdamThreads, step_ctas_per_sm(BITS)) adamw_kernel(char* ws, Layout lay, Rates r) {
+    constexpr int S = BITS / 8;
     ptx::grid_handover();
     Control* control = reinterpret_cast<Control*>(ws);
     __shared__ Tensor table[kTable];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31;
     const int32_t skip = control->skip;
     if (!skip) {
-        const float2 factor = pair(control->factor);
         const double t = (double)(control->step + 1);
         const float lr = r.lr_device ? *r.lr_device : r.lr;
         const float correction1 = -expm1f((float)(t * r.log_beta1)), correction2 = -expm1f((float)(t * r.log_beta2));
-        const float2 root2 = pair(rsqrtf(correction2)), eps = pair(r.eps);
-        const float2 beta1 = pair(r.beta1), new1 = pair(r.one_minus_beta1), beta2 = pair(r.beta2), new2 = pair(r.one_minus_beta2), one = pair(r.one);
-        for_chunks(ws, lay, table, [&](int begin, int end) {
-            // A block is fetched while the one before is computed: with 8-bit states, whose arithmetic takes as long as the memory does.
-            constexpr bool kAhead = BITS == 8;
+        const Formula f{pair(control->factor), pair(r.beta1), pair(r.one_minus_beta1), pair(r.beta2), pair(r.one_minus_beta2), pair(r.one), pair(r.eps),
+                        pair(rsqrtf(correction2))};
+        // A block with 8-bit states is fetched while the one before is computed: its arithmetic takes as long as the memory does.
+        constexpr bool kAhead = BITS == 8;
+        for_chunks(ws, lay, table, [&](int64_t first, int count) {
             Fetched<BITS> next;
-            int ahead = 0;
-            auto fetch = [&](int c) {
-                ahead = tensor_of(table, ahead, c);
-                const Tensor& x = table[ahead];
-                next.base = (int64_t)(c - x.first_chunk) * kChunk + warp * kBlock;
-                const int left = block_elements(x.numel - next.base);
-                if (left == 0) return;
-                if (BITS == 8) { next.m_scale = x.m_scale[next.base / kBlock]; next.v_scale = x.v_scale[next.base / kBlock]; }
+            bool fetched = false;
+            auto fetch = [&](const Tensor& x, int64_t base) {
+                const int64_t at = base + lane * 4;
+                const int grad_dtype = GRAD == kMixed ? x.grad_dtype : GRAD, param_dtype = PARAM == kMixed ? x.param_dtype : PARAM;
+                const char *m = (const char*)x.m + at * S, *v = (const char*)x.v + at * S;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int first = h * kRun + lane * 4;
-                    const int64_t at = next.base + first;
-                    next.g[h] = load_typed4(x.grad, at, first, left, GRAD == kMixed ? x.grad_dtype : GRAD);
-                    next.p[h] = x.master ? load_raw4<4>(x.master, at, first, left) : load_typed4(x.param, at, first, left, PARAM == kMixed ? x.param_dtype : PARAM);
-                    next.m[h] = load_raw4<BITS / 8>(x.m, at, first, left);
-                    next.v[h] = load_raw4<BITS / 8>(x.v, at, first, left);
+                    next.g[h] = grad_dtype == EQL_FP32 ? load_raw4<4>((const float*)x.grad + at + h * kRun) : load_raw4<2>((const uint16_t*)x.grad + at + h * kRun);
+                    next.m[h] = load_raw4<S>(m + h * kRun * S);
+                    next.v[h] = load_raw4<S>(v + h * kRun * S);
                 }
+                if (x.master) {
+                    next.p[0] = load_raw4<4>(x.master + at);
+                    next.p[1] = load_raw4<4>(x.master + at + kRun);
+                } else {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        next.p[h] = param_dtype == EQL_FP32 ? load_raw4<4>((const float*)x.param + at + h * kRun) : load_raw4<2>((const uint16_t*)x.param + at + h * kRun);
+                }
+                if (BITS == 8) { next.m_scale = x.m_scale[base / kBlock]; next.v_scale = x.v_scale[base / kBlock]; }
             };
-            int which = 0;
-            if (kAhead) fetch(begin);
-            for (int c = begin; c < end; ++c) {
-                if (!kAhead) fetch(c);
-                const Fetched<BITS> now = next;
-                which = kAhead ? tensor_of(table, which, c) : ahead;
-                if (kAhead && c + 1 < end) fetch(c + 1);
-                const Tensor& x = table[which];
-                const int left = block_elements(x.numel - now.base);
-                if (left == 0) continue;
+            for (int i = 0; i < count; ++i) {
+                const Tensor& x = table[i];
+                const Block block(x, first + (int64_t)i * gridDim.x);
+                const bool whole = block.count == kBlock;
+                if (whole && !fetched) fetch(x, block.base);
+                Fetched<BITS> now = next;
+                fetched = false;
+                if (kAhead && i + 1 < count) {
+                    const Block after(table[i + 1], first + (int64_t)(i + 1) * gridDim.x);
+                    fetched = after.count == kBlock;
+                    if (fetched) fetch(table[i + 1], after.base);
+                }
+                if (block.count == 0) continue;
                 const float rate = lr * x.lr_scale;
                 const float2 keep = pair(1.0f - rate * x.weight_decay), size = pair(__fdividef(-rate, correction1));
+                if (!whole) {
+                    update_end<BITS>(f, x, block.base, block.count, keep, size);
+                    continue;
+                }
                 const int grad_dtype = GRAD == kMixed ? x.grad_dtype : GRAD, param_dtype = PARAM == kMixed ? x.param_dtype : PARAM;
-                const int64_t block = now.base / kBlock;
-                float2 g[4], m[4], v[4], p[4];
+                float2 value[4];
+                update<BITS>(f, now, grad_dtype, x.master ? (int)EQL_FP32 : param_dtype, keep, size, value);
+                const int64_t at = block.base + lane * 4;
+                if (x.master) {
+                    store_raw4<4>(x.master + at, narrow4(value, EQL_FP32));
+                    store_raw4<4>(x.master + at + kRun, narrow4(value + 2, EQL_FP32));
+                }
+                char *m = (char*)x.m + at * S, *v = (char*)x.v + at * S;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    widen4(now.g[h], grad_dtype, g + 2 * h);
-                    if (x.master) widen4(now.p[h], EQL_FP32, p + 2 * h);
-                    else widen4(now.p[h], param_dtype, p + 2 * h);
-                    if (BITS == 32) {
-                        widen4(now.m[h], EQL_FP32, m + 2 * h);
-                        widen4(now.v[h], EQL_FP32, v + 2 * h);
-                    } else {
-                        decode4<__NV_E4M3>(now.m[h].x, pair(now.m_scale), m + 2 * h);
-                        decode4<__NV_E5M2>(now.v[h].x, pair(now.v_scale), v + 2 * h);
-                    }
+                    if (param_dtype == EQL_FP32) store_raw4<4>((float*)x.param + at + h * kRun, narrow4(value + 2 * h, EQL_FP32));
+                    else store_raw4<2>((uint16_t*)x.param + at + h * kRun, narrow4(value + 2 * h, param_dtype));
+                    store_raw4<S>(m + h * kRun * S, now.m[h]);
+                    store_raw4<S>(v + h * kRun * S, now.v[h]);
                 }
-            float most_m = 0.0f, most_v = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float2 gs = mul2(g[j], factor);
-                m[j] = fma2(mul2(m[j], beta1), one, mul2(gs, new1));
-                v[j] = fma2(mul2(v[j], beta2), one, mul2(mul2(gs, gs), new2));
-                if (BITS == 8) {
-                    most_m = fmaxf(most_m, fmaxf(fabsf(m[j].x), fabsf(m[j].y)));
-                    most_v = fmaxf(most_v, fmaxf(v[j].x, v[j].y));
-                }
-                float2 root;
-                asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(root.x) : "f"(v[j].x));
-                asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(root.y) : "f"(v[j].y));
-                p[j] = fma2(mul2(size, m[j]), reciprocal(fma2(root, root2, eps)), mul2(p[j], keep));
-            }
-            float2 qm[4], qv[4];
-            if (BITS == 8) {
-                most_m = warp_max(most_m);
-                most_v = warp_max(most_v);
-                const bool fine_m = !(most_m < kTiny), fine_v = !(most_v < kTiny);
-                // the block's four divisions, each in another lane: the inverse scales of m and v, and the scales
-                const bool of_v = lane & 1, scale = lane & 2;
-                const float most = of_v ? most_v : most_m, top = of_v ? kE5m2Max : kE4m3Max;
-                const float ratio = (of_v ? fine_v : fine_m) ? __fdiv_rn(scale ? most : top, scale ? top : most) : 0.0f;
-                const float2 im = pair(__shfl_sync(0xffffffffu, ratio, 0)), iv = pair(__shfl_sync(0xffffffffu, ratio, 1));
-                float smallest = kE5m2Least;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    qm[j] = mul2(m[j], im);
-                    qv[j] = mul2(v[j], iv);
-                    smallest = fminf(smallest, fminf(qv[j].x, qv[j].y));
-                }
-                if (smallest < kE5m2Least && fine_v) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if (v[j].x > 0.0f) qv[j].x = fmaxf(qv[j].x, kE5m2Least);
-                        if (v[j].y > 0.0f) qv[j].y = fmaxf(qv[j].y, kE5m2Least);
-                    }
-                }
-                if (lane == 2) x.m_scale[block] = ratio;
-                if (lane == 3) x.v_scale[block] = ratio;
-            }
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int first = h * kRun + lane * 4;
-                const int64_t at = now.base + first;
-                if (x.master) store_typed4(x.master, at, first, left, EQL_FP32, p + 2 * h);
-                store_typed4(x.param, at, first, left, param_dtype, p + 2 * h);
-                if (BITS == 32) {
-                    store_typed4(x.m, at, first, left, EQL_FP32, m + 2 * h);
-                    store_typed4(x.v, at, first, left, EQL_FP32, v + 2 * h);
-                } else {
-                    store_raw4<1>(x.m, at, first, left, make_uint4(encode4<__NV_E4M3>(qm + 2 * h), 0u, 0u, 0u));
-                    store_raw4<1>(x.v, at, first, left, make_uint4(encode4<__NV_E5M2>(qv + 2 * h), 0u, 0u, 0u));
-                }
-            }
+                if (BITS == 8 && lane == 2) x.m_scale[block.base / kBlock] = now.m_scale;
+                if (BITS == 8 && lane == 3) x.v_scale[block.base / kBlock] = now.v_scale;
             }
         });
     }
@@ -362,37 +426,44 @@ __global__ void __launch_bounds__(kAdamThreads, kNormCtasPerSm) grad_norm_kernel
     __shared__ Tensor table[kTable];
     __shared__ double shared[kAdamThreads / 32];
     __shared__ bool last;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31;
     double sums[4] = {};
-    for_chunks(ws, lay, table, [&](int begin, int end) {
-        int which = 0;
-        for (int c = begin; c < end; c += kNormUnroll) {
+    auto add = [&](const uint4& u, int dtype) {
+        float2 f[2];
+        widen4(u, dtype, f);
+        sums[0] = fma((double)f[0].x, (double)f[0].x, sums[0]);
+        sums[1] = fma((double)f[0].y, (double)f[0].y, sums[1]);
+        sums[2] = fma((double)f[1].x, (double)f[1].x, sums[2]);
+        sums[3] = fma((double)f[1].y, (double)f[1].y, sums[3]);
+    };
+    for_chunks(ws, lay, table, [&](int64_t first, int count) {
+        for (int i0 = 0; i0 < count; i0 += kNormUnroll) {
             uint4 u[kNormUnroll][2];
-            int dtype[kNormUnroll];
 #pragma unroll
             for (int i = 0; i < kNormUnroll; ++i) {
-                dtype[i] = GRAD == kMixed ? (int)EQL_FP32 : GRAD;
                 u[i][0] = u[i][1] = make_uint4(0u, 0u, 0u, 0u);
-                if (c + i >= end) continue;
-                which = tensor_of(table, which, c + i);
-                const Tensor& x = table[which];
-                if (GRAD == kMixed) dtype[i] = x.grad_dtype;
-                const int64_t base = (int64_t)(c + i - x.first_chunk) * kChunk + warp * kBlock;
-                const int left = block_elements(x.numel - base);
+                if (i0 + i >= count) continue;
+                const Tensor& x = table[i0 + i];
+                const Block block(x, first + (int64_t)(i0 + i) * gridDim.x);
+                const int size = (GRAD == kMixed ? x.grad_dtype : GRAD) == EQL_FP32 ? 4 : 2;
+                const char* g = (const char*)x.grad + (block.base + lane * 4) * size;
+                if (block.count == kBlock) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) u[i][h] = load_typed4(x.grad, base + h * kRun + lane * 4, h * kRun + lane * 4, left, dtype[i]);
+                    for (int h = 0; h < 2; ++h) u[i][h] = size == 4 ? load_raw4<4>(g + h * kRun * 4) : load_raw4<2>(g + h * kRun * 2);
+                } else {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int mine = block.count - h * kRun - lane * 4;
+                        u[i][h] = size == 4 ? load_some4<4>(g + h * kRun * 4, mine) : load_some4<2>(g + h * kRun * 2, mine);
+                    }
+                }
             }
 #pragma unroll
-            for (int i = 0; i < kNormUnroll; ++i)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    float2 f[2];
-                    widen4(u[i][h], dtype[i], f);
-                    sums[0] = fma((double)f[0].x, (double)f[0].x, sums[0]);
-                    sums[1] = fma((double)f[0].y, (double)f[0].y, sums[1]);
-                    sums[2] = fma((double)f[1].x, (double)f[1].x, sums[2]);
-                    sums[3] = fma((double)f[1].y, (double)f[1].y, sums[3]);
-                }
+            for (int i = 0; i < kNormUnroll; ++i) {
+                const int dtype = GRAD != kMixed ? GRAD : table[i0 + i < count ? i0 + i : i0].grad_dtype;
+                add(u[i][0], dtype);
+                add(u[i][1], dtype);
+            }
         }
     });
     double sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
@@ -573,7 +644,7 @@ eql_status_t eqlinear_adamw(eqlinear_adamw_t* opt, const eql_adamw_tensor_t* ten
     for (int i = 0; i < count; ++i) {
         const eql_adamw_tensor_t& t = tensors[i];
         table[i] = Tensor{t.param, (float*)t.master, t.grad, t.exp_avg, t.exp_avg_sq, t.exp_avg_scale, t.exp_avg_sq_scale, t.numel, (int32_t)chunk,
-                          (int32_t)chunks_of(t.numel), t.param_dtype, t.grad_dtype, t.weight_decay, t.lr_scale};
+                          t.param_dtype, t.grad_dtype, t.weight_decay, t.lr_scale, 0};
         for (int64_t k = chunks_of(t.numel); k > 0; --k) chunk_tensor[chunk++] = i;
     }
     cudaError_t e = cudaMemcpyAsync(workspace, image, lay.total, cudaMemcpyHostToDevice, s);
@@ -609,7 +680,7 @@ eql_status_t eqlinear_adamw_step(eqlinear_adamw_t opt, double lr, double beta1, 
     if (!((float)eps >= FLT_MIN) || !std::isfinite((float)eps)) return EQL_ERR_INVALID_ARG;
     if (!aligned(lr_device, 4)) return EQL_ERR_ALIGNMENT;
     const Rates r{(float)lr, (float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps, 1.0f, std::log(beta1), std::log(beta2), lr_device};
-    const int64_t most = (int64_t)opt->num_sms * kStepCtasPerSm;
+    const int64_t most = (int64_t)opt->num_sms * step_ctas_per_sm(opt->state_bits);
     const unsigned grid = (unsigned)std::max<int64_t>(1, std::min(opt->lay.n_chunks, most));
     const auto kernel = opt->state_bits == 8 ? step_kernel<8>(opt->grad_dtype, opt->param_dtype) : step_kernel<32>(opt->grad_dtype, opt->param_dtype);
     cudaError_t e = launch_overlapped(kernel, dim3(grid), dim3(kAdamThreads), 0, (cudaStream_t)stream, opt->ws, opt->lay, r);
