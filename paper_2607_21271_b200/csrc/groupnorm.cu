@@ -241,9 +241,11 @@ __global__ void __launch_bounds__(kThreads) channel_sums_kernel(NormShape s, Ran
     float2 sum = make_float2(0.0f, 0.0f);
     if (channel < s.C) {
         const int piece0 = channel * s.T / size, pieces = ((channel + 1) * s.T - 1) / size - piece0 + 1;
-        for (int i = threadIdx.x >> 3; i < g.ranges * pieces; i += kThreads / 8) {
-            const int range = i / pieces, piece = piece0 + i % pieces;
-            sum = add2(sum, reinterpret_cast<const float2*>(g.partials)[((b * g.ranges + range) * g.pieces + piece) * g.parts + channel - piece * size / s.T]);
+        for (int piece = piece0; piece < piece0 + pieces; ++piece) {
+            const float2* from = reinterpret_cast<const float2*>(g.partials) + (b * g.ranges * g.pieces + piece) * g.parts + channel - piece * size / s.T;
+            const int64_t step = (int64_t)g.pieces * g.parts;
+#pragma unroll 8
+            for (int range = threadIdx.x >> 3; range < g.ranges; range += kThreads / 8) sum = add2(sum, from[range * step]);
         }
     }
     shared[threadIdx.x] = sum;
@@ -320,11 +322,10 @@ __global__ void __launch_bounds__(kThreads) parameter_sums_kernel(const float2* 
     __shared__ float2 shared[kThreads];
     const int channel = blockIdx.x * 8 + (threadIdx.x & 7);
     float2 sum = make_float2(0.0f, 0.0f);
-    if (channel < C)
-        for (int64_t i = threadIdx.x >> 3; i < count; i += kThreads / 8) {
-            const float2 v = parts[i * C + channel];
-            sum.x += v.x; sum.y += v.y;
-        }
+    if (channel < C) {
+#pragma unroll 8
+        for (int64_t i = threadIdx.x >> 3; i < count; i += kThreads / 8) sum = add2(sum, parts[i * C + channel]);
+    }
     shared[threadIdx.x] = sum;
     __syncthreads();
     if (threadIdx.x < 8 && channel < C) {
