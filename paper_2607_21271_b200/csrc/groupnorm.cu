@@ -148,46 +148,59 @@ __global__ void __launch_bounds__(kThreads) group_moments_kernel(NormShape s, Ra
     }
 }
 
-// What a thread keeps of its column: the group's mean and rstd, gamma and beta.
-template <typename IO>
+// What a thread keeps of its column, N: see Runs.
+template <typename IO, int N>
 struct Column {
-    static constexpr int V = NormIo<IO>::kVec;
-    float2 mean[V / 2], rstd[V / 2], gamma[V / 2], beta[V / 2];
+    static constexpr int V = NormIo<IO>::kVec, P = V / 2;
+    using R = Runs<N, P>;
+    R mean, rstd, scale, beta;                                // scale: rstd * gamma
     __device__ __forceinline__ Column(const NormShape& s, const float2* stats, const IO* gammas, const IO* betas, int64_t b, int vector) {
+        const int channel = vector * V / s.T, group = vector * V / s.width;
+        R::each(channel, vector * V - channel * s.T, s.T, [&](int e, int c) {
+            scale.set(e, gammas ? NormIo<IO>::one(gammas, c) : 1.0f);
+            beta.set(e, betas ? NormIo<IO>::one(betas, c) : 0.0f);
+        });
+        R::each(group, vector * V - group * s.width, s.width, [&](int e, int g) {
+            const float2 st = stats[b * s.groups + g];
+            mean.set(e, st.x);
+            rstd.set(e, st.y);
+        });
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int e = vector * V + j, channel = e / s.T;
-            const float2 st = stats[b * s.groups + e / s.width];
-            (&mean[j / 2].x)[j % 2] = st.x;
-            (&rstd[j / 2].x)[j % 2] = st.y;
-            (&gamma[j / 2].x)[j % 2] = gammas ? NormIo<IO>::one(gammas, channel) : 1.0f;
-            (&beta[j / 2].x)[j % 2] = betas ? NormIo<IO>::one(betas, channel) : 0.0f;
+        for (int j = 0; j < N; ++j) scale.v[j] = mul2(scale.v[j], rstd.v[j]);
+    }
+    // x - mean and dz of a vector
+    template <int ACT>
+    __device__ __forceinline__ void gradient(const uint4* u, float2* xc, float2* dz) const {
+        NormIo<IO>::widen(u[0], xc);
+        NormIo<IO>::widen(u[1], dz);
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            xc[j] = sub2(xc[j], mean.of(j));
+            if (ACT != EQL_ACT_NONE) dz[j] = mul2(dz[j], slope<ACT>(fma2(xc[j], scale.of(j), beta.of(j))));
         }
     }
 };
 
-template <typename IO, int ACT>
+template <typename IO, int ACT, int N>
 __global__ void __launch_bounds__(kThreads) apply_kernel(NormShape s, Ranges g, const uint4* x, const IO* gamma, const IO* beta,
                                                          const int32_t* lengths, uint4* y) {
     constexpr int V = NormIo<IO>::kVec;
     ptx::grid_handover();
     const Place p = place(s, g, lengths, gridDim.x - 1 - blockIdx.x);
     if (!p.active || p.lane >= p.rows) return;
-    Column<IO> c(s, reinterpret_cast<const float2*>(g.groups), gamma, beta, p.b, p.vector);
-#pragma unroll
-    for (int j = 0; j < V / 2; ++j) c.gamma[j] = mul2(c.gamma[j], c.rstd[j]);
+    const Column<IO, N> c(s, reinterpret_cast<const float2*>(g.groups), gamma, beta, p.b, p.vector);
     const int64_t at = (p.b * s.S + p.row0 + p.lane) * s.vectors + p.vector, step = (int64_t)p.lanes * s.vectors;
     walk<1>(p.rows_of(p.lane), [&](int i, uint4* u) { u[0] = x[at + i * step]; },
             [&](int i, const uint4* u) {
                 float2 f[V / 2];
                 NormIo<IO>::widen(u[0], f);
 #pragma unroll
-                for (int j = 0; j < V / 2; ++j) f[j] = activate<ACT>(fma2(sub2(f[j], c.mean[j]), c.gamma[j], c.beta[j]));
+                for (int j = 0; j < V / 2; ++j) f[j] = activate<ACT>(fma2(sub2(f[j], c.mean.of(j)), c.scale.of(j), c.beta.of(j)));
                 y[at + i * step] = NormIo<IO>::narrow(f);
             });
 }
 
-template <typename IO, int ACT>
+template <typename IO, int ACT, int N>
 __global__ void __launch_bounds__(kThreads) part_sums_kernel(NormShape s, Ranges g, const uint4* x, const uint4* dy, const IO* gamma, const IO* beta,
                                                              const int32_t* lengths, const float* stats) {
     constexpr int V = NormIo<IO>::kVec;
@@ -196,20 +209,20 @@ __global__ void __launch_bounds__(kThreads) part_sums_kernel(NormShape s, Ranges
     const Place p = place(s, g, lengths, blockIdx.x);
     float2 db[V / 2] = {}, dg[V / 2] = {};
     if (p.active && p.lane < p.rows) {
-        const Column<IO> c(s, reinterpret_cast<const float2*>(stats), gamma, beta, p.b, p.vector);
+        const Column<IO, N> c(s, reinterpret_cast<const float2*>(stats), gamma, beta, p.b, p.vector);
         const int64_t at = (p.b * s.S + p.row0 + p.lane) * s.vectors + p.vector, step = (int64_t)p.lanes * s.vectors;
         walk<2>(p.rows_of(p.lane), [&](int i, uint4* u) { u[0] = x[at + i * step]; u[1] = dy[at + i * step]; },
                 [&](int, const uint4* u) {
-                    float2 f[V / 2], d[V / 2];
-                    NormIo<IO>::widen(u[0], f);
-                    NormIo<IO>::widen(u[1], d);
+                    float2 xc[V / 2], dz[V / 2];
+                    c.template gradient<ACT>(u, xc, dz);
 #pragma unroll
                     for (int j = 0; j < V / 2; ++j) {
-                        const float2 xh = mul2(sub2(f[j], c.mean[j]), c.rstd[j]), dz = mul2(d[j], slope<ACT>(fma2(xh, c.gamma[j], c.beta[j])));
-                        db[j] = add2(db[j], dz);
-                        dg[j] = fma2(dz, xh, dg[j]);
+                        db[j] = add2(db[j], dz[j]);
+                        dg[j] = fma2(dz[j], xc[j], dg[j]);
                     }
                 });
+#pragma unroll
+        for (int j = 0; j < V / 2; ++j) dg[j] = mul2(dg[j], c.rstd.of(j));
     }
     if (p.active) {
 #pragma unroll
@@ -286,33 +299,35 @@ __global__ void __launch_bounds__(kThreads) group_sums_kernel(NormShape s, Range
     }
 }
 
-template <typename IO, int ACT>
+template <typename IO, int ACT, int N>
 __global__ void __launch_bounds__(kThreads) apply_gradient_kernel(NormShape s, Ranges g, const uint4* x, const uint4* dy, const IO* gamma, const IO* beta,
                                                                   const int32_t* lengths, const float* stats, uint4* dx) {
     constexpr int V = NormIo<IO>::kVec;
     ptx::grid_handover();
     const Place p = place(s, g, lengths, gridDim.x - 1 - blockIdx.x);
     if (!p.active || p.lane >= p.rows) return;
-    const Column<IO> c(s, reinterpret_cast<const float2*>(stats), gamma, beta, p.b, p.vector);
-    float2 off1[V / 2], off2[V / 2];
+    const Column<IO, N> c(s, reinterpret_cast<const float2*>(stats), gamma, beta, p.b, p.vector);
+    // dx = dz * (rstd * gamma) - (x - mean) * (rstd * rstd * second) - rstd * first
+    Runs<N, V / 2> off1, off2;
+    const int group = p.vector * V / s.width;
+    Runs<N, V / 2>::each(group, p.vector * V - group * s.width, s.width, [&](int e, int k) {
+        const float2 v = reinterpret_cast<const float2*>(g.groups)[p.b * s.groups + k];
+        off1.set(e, -v.x);
+        off2.set(e, -v.y);
+    });
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const float2 v = reinterpret_cast<const float2*>(g.groups)[p.b * s.groups + (p.vector * V + j) / s.width];
-        (&off1[j / 2].x)[j % 2] = -v.x;
-        (&off2[j / 2].x)[j % 2] = -v.y;
+    for (int j = 0; j < N; ++j) {
+        off1.v[j] = mul2(off1.v[j], c.rstd.v[j]);
+        off2.v[j] = mul2(mul2(off2.v[j], c.rstd.v[j]), c.rstd.v[j]);
     }
     const int64_t at = (p.b * s.S + p.row0 + p.lane) * s.vectors + p.vector, step = (int64_t)p.lanes * s.vectors;
     walk<2>(p.rows_of(p.lane), [&](int i, uint4* u) { u[0] = x[at + i * step]; u[1] = dy[at + i * step]; },
             [&](int i, const uint4* u) {
-                float2 f[V / 2], d[V / 2];
-                NormIo<IO>::widen(u[0], f);
-                NormIo<IO>::widen(u[1], d);
+                float2 xc[V / 2], dz[V / 2];
+                c.template gradient<ACT>(u, xc, dz);
 #pragma unroll
-                for (int j = 0; j < V / 2; ++j) {
-                    const float2 xh = mul2(sub2(f[j], c.mean[j]), c.rstd[j]), dz = mul2(d[j], slope<ACT>(fma2(xh, c.gamma[j], c.beta[j])));
-                    f[j] = mul2(c.rstd[j], fma2(xh, off2[j], fma2(c.gamma[j], dz, off1[j])));
-                }
-                dx[at + i * step] = NormIo<IO>::narrow(f);
+                for (int j = 0; j < V / 2; ++j) xc[j] = fma2(xc[j], off2.of(j), fma2(dz[j], c.scale.of(j), off1.of(j)));
+                dx[at + i * step] = NormIo<IO>::narrow(xc);
             });
 }
 
@@ -411,7 +426,8 @@ cudaError_t run_ranges(const NormShape& s, const Ranges& g, eql_dtype_t dtype, c
         if (err == cudaSuccess) err = launch_overlapped(group_moments_kernel, dim3((unsigned)units), dim3(kThreads), 0, st, s, g, NormIo<IO>::kVec, lengths, stats);
         if (err != cudaSuccess) return err;
         return dispatch_act(s.act, [&](auto act) {
-            return launch_overlapped(apply_kernel<IO, decltype(act)::value>, dim3((unsigned)grid), dim3(kThreads), 0, st, s, g, (const uint4*)x,
+            constexpr int ACT = decltype(act)::value, V = NormIo<IO>::kVec;
+            return launch_overlapped(runs_of(s.T, V) == 1 ? apply_kernel<IO, ACT, 1> : runs_of(s.T, V) == 2 ? apply_kernel<IO, ACT, 2> : apply_kernel<IO, ACT, V / 2>, dim3((unsigned)grid), dim3(kThreads), 0, st, s, g, (const uint4*)x,
                                      (const IO*)gamma, (const IO*)beta, lengths, (uint4*)y);
         });
     });
@@ -423,8 +439,9 @@ cudaError_t run_ranges_gradient(const NormShape& s, const Ranges& g, eql_dtype_t
     return dispatch_io(dtype, [&](auto io) {
         using IO = decltype(io);
         return dispatch_act(s.act, [&](auto act) {
-            constexpr int ACT = decltype(act)::value;
-            cudaError_t err = launch_overlapped(part_sums_kernel<IO, ACT>, dim3((unsigned)grid), dim3(kThreads), 0, st, s, g, (const uint4*)x,
+            constexpr int ACT = decltype(act)::value, V = NormIo<IO>::kVec;
+            const int runs = runs_of(s.T, V);
+            cudaError_t err = launch_overlapped(runs == 1 ? part_sums_kernel<IO, ACT, 1> : runs == 2 ? part_sums_kernel<IO, ACT, 2> : part_sums_kernel<IO, ACT, V / 2>, dim3((unsigned)grid), dim3(kThreads), 0, st, s, g, (const uint4*)x,
                                                 (const uint4*)dy, (const IO*)gamma, (const IO*)beta, lengths, stats);
             if (err == cudaSuccess)
                 err = launch_overlapped(channel_sums_kernel, dim3((unsigned)(s.B * ((s.C + 7) / 8))), dim3(kThreads), 0, st, s, g, NormIo<IO>::kVec);
@@ -432,7 +449,7 @@ cudaError_t run_ranges_gradient(const NormShape& s, const Ranges& g, eql_dtype_t
                 err = launch_overlapped(group_sums_kernel<IO>, dim3((unsigned)((units + kThreads / 32 - 1) / (kThreads / 32))), dim3(kThreads), 0, st, s, g,
                                         (const IO*)gamma, lengths);
             if (err == cudaSuccess)
-                err = launch_overlapped(apply_gradient_kernel<IO, ACT>, dim3((unsigned)grid), dim3(kThreads), 0, st, s, g, (const uint4*)x,
+                err = launch_overlapped(runs == 1 ? apply_gradient_kernel<IO, ACT, 1> : runs == 2 ? apply_gradient_kernel<IO, ACT, 2> : apply_gradient_kernel<IO, ACT, V / 2>, dim3((unsigned)grid), dim3(kThreads), 0, st, s, g, (const uint4*)x,
                                         (const uint4*)dy, (const IO*)gamma, (const IO*)beta, lengths, stats, (uint4*)dx);
             return err == cudaSuccess ? launch_parameter_sums(g.channels, s.B, s.C, dgamma, dbeta, st) : err;
         });

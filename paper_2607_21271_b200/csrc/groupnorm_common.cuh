@@ -170,6 +170,33 @@ struct RunningMoments {
 };
 __device__ __forceinline__ float rstd_of(const Moments& v, float eps) { return rsqrtf((v.n > 0.0f ? __fdividef(v.m2, v.n) : 0.0f) + eps); }
 
+// What belongs to the elements of a vector in N equal runs: channels and groups begin where runs do.  N = 1 where the vector is of one
+// channel, 2 where it is of two of half its length each, all pairs otherwise (and then each element for itself).
+template <int N, int P>
+struct Runs {
+    float2 v[N];
+    __device__ __forceinline__ const float2& of(int pair_index) const { return v[pair_index * N / P]; }
+    __device__ __forceinline__ float2& of(int pair_index) { return v[pair_index * N / P]; }
+    __device__ __forceinline__ void set(int entry, float value) {         // entry of kEntries
+        if (N < P) v[entry] = pair(value);
+        else (&v[entry / 2].x)[entry % 2] = value;
+    }
+    static constexpr int kEntries = N < P ? N : 2 * P, kLength = 2 * P / kEntries;      // (an entry's elements)
+    // set(entry, its channel), and the same for groups, for the vector whose first element is element `at` of the channel or group `first`
+    template <typename Set>
+    static __device__ __forceinline__ void each(int first, int at, int length, Set&& set) {
+#pragma unroll
+        for (int e = 0; e < kEntries; ++e) {
+            set(e, first);
+            at += kLength;
+            if (at >= length) { at -= length; ++first; }
+        }
+    }
+};
+// The N above for tuples of T elements, and the neighbouring elements of a vector that are of one channel (whatever the vector).
+constexpr int runs_of(int T, int V) { return T % V == 0 ? 1 : T % (V / 2) == 0 ? 2 : V / 2; }
+constexpr int run_length(int T, int V) { return T % V == 0 ? V : T % (V / 2) == 0 ? V / 2 : V % T == 0 ? T : 1; }
+
 __device__ __forceinline__ int64_t positions_of(const int32_t* lengths, int64_t b, int64_t S) {
     if (!lengths) return S;
     const int64_t n = lengths[b];

@@ -133,44 +133,29 @@ __device__ __forceinline__ Moments moments_of(float count, int entries, At&& at)
     return Moments{count, middle + mean, m2 < 0.0f ? 0.0f : m2};
 }
 
-// The groups of a vector's elements, relative to its first element's: three bits each.
-template <int N, int V>
+// The groups of a vector's runs, relative to its first element's: three bits each.
+template <typename R>
 __device__ __forceinline__ unsigned group_steps(const NormShape& s, int in_group) {
     unsigned steps = 0;
-    if (N > 1) {
-        int step = 0;
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            steps |= step << (3 * j);
-            if (++in_group == s.width) { in_group = 0; ++step; }
-        }
-    }
+    if (R::kEntries > 1) R::each(0, in_group, s.width, [&](int e, int step) { steps |= (unsigned)step << (3 * e); });
     return steps;
 }
-// What belongs to the elements of a vector: N = 1 where they are of one channel (and so of one group), else a pair for each two.
-// set(element, channel) for every element, and set(element, group) with the steps above.
-template <int N, int V, typename Set>
-__device__ __forceinline__ void each_channel(const NormShape& s, const ResidentNorm& r, const Post& p, Set&& set) {
-    int channel = r.tuple(p.column * V), in_channel = p.column * V - channel * s.T;
-    channel += p.first_group * (s.C / s.groups);
-#pragma unroll
-    for (int j = 0; j < (N == 1 ? 1 : V); ++j) {
-        set(j, channel);
-        if (++in_channel == s.T) { in_channel = 0; ++channel; }
-    }
-}
-template <int N, int V, typename Set>
+template <typename R, typename Set>
 __device__ __forceinline__ void each_group(unsigned steps, const float2* first, Set&& set) {
 #pragma unroll
-    for (int j = 0; j < (N == 1 ? 1 : V); ++j) set(j, first[steps >> (3 * j) & 7u]);
+    for (int e = 0; e < R::kEntries; ++e) set(e, first[steps >> (3 * e) & 7u]);
 }
-template <int N> __device__ __forceinline__ float2 of_pair(const float2 (&v)[N], int j) { return N == 1 ? v[0] : v[j]; }
-template <int N> __device__ __forceinline__ void put(float2 (&v)[N], int j, float value) {
-    if (N == 1) v[0] = pair(value);
-    else (&v[j / 2].x)[j % 2] = value;
+// Gamma and beta of a thread's column.
+template <typename IO, typename R>
+__device__ __forceinline__ void parameters(const NormShape& s, const ResidentNorm& r, const Post& p, const IO* gammas, const IO* betas, R* gamma, R* beta) {
+    const int first = r.tuple(p.column * NormIo<IO>::kVec), block = p.first_group * (s.C / s.groups);
+    R::each(first, p.column * NormIo<IO>::kVec - first * s.T, s.T, [&](int e, int channel) {
+        gamma->set(e, p.active && gammas ? NormIo<IO>::one(gammas, block + channel) : 1.0f);
+        beta->set(e, p.active && betas ? NormIo<IO>::one(betas, block + channel) : 0.0f);
+    });
 }
 
-// N: see each_element.
+// N: see Runs.
 template <typename IO, int ACT, int N, int THREADS, int CTAS>
 __global__ void __launch_bounds__(THREADS, CTAS) resident_norm_kernel(NormShape s, ResidentNorm r, const uint4* x, const IO* gammas, const IO* betas,
                                                                       const int32_t* lengths, uint4* y, float2* stats) {
@@ -190,14 +175,11 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_norm_kernel(NormShape 
         const uint4* from = x + p.at(s, p.b);
         refill(0, mine, [](int) {}, [&](int i) { copy_async16(slot + i * pitch, from); from += step; });
     }
-    float2 gamma[N], beta[N];
-    each_channel<N, V>(s, r, p, [&](int j, int channel) {
-        put(gamma, j, p.active && gammas ? NormIo<IO>::one(gammas, channel) : 1.0f);
-        put(beta, j, p.active && betas ? NormIo<IO>::one(betas, channel) : 0.0f);
-    });
+    Runs<N, P> gamma, beta;
+    parameters(s, r, p, gammas, betas, &gamma, &beta);
     const bool whole = N == 1 || s.width % V == 0;            // a vector lies in one group
     const int group = r.width(p.column * V);                  // of the block, that of the first element
-    const unsigned steps = group_steps<N, V>(s, p.column * V - group * s.width);
+    const unsigned steps = group_steps<Runs<N, P>>(s, p.column * V - group * s.width);
     int round = 0;
     for (int64_t b = p.b; b < s.B; b += r.instances, ++round) {
         RunningMoments<P> moments;
@@ -277,13 +259,13 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_norm_kernel(NormShape 
             }
             __syncthreads();
         }
-        float2 mean[N], scale[N];
-        each_group<N, V>(steps, m.result + group, [&](int j, float2 v) {
-            put(mean, j, v.x);
-            put(scale, j, v.y);
+        Runs<N, P> mean, scale;
+        each_group<Runs<N, P>>(steps, m.result + group, [&](int e, float2 v) {
+            mean.set(e, v.x);
+            scale.set(e, v.y);
         });
 #pragma unroll
-        for (int j = 0; j < N; ++j) scale[j] = mul2(scale[j], gamma[j]);
+        for (int j = 0; j < N; ++j) scale.v[j] = mul2(scale.v[j], gamma.v[j]);
         // every slot, once used, takes the next instance's vector
         const Rows next = lengths || b + r.instances >= s.B ? Rows(s, r, p, lengths, b + r.instances) : rows;
         const int count = p.active ? next.of(p.lane) : 0;
@@ -293,7 +275,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_norm_kernel(NormShape 
             float2 f[P];
             NormIo<IO>::widen(slot[i * pitch], f);
 #pragma unroll
-            for (int j = 0; j < P; ++j) f[j] = activate<ACT>(fma2(sub2(f[j], of_pair(mean, j)), of_pair(scale, j), of_pair(beta, j)));
+            for (int j = 0; j < P; ++j) f[j] = activate<ACT>(fma2(sub2(f[j], mean.of(j)), scale.of(j), beta.of(j)));
             *to = NormIo<IO>::narrow(f);
             to += step;
         };
@@ -329,13 +311,10 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
             from_dy += step;
         });
     }
-    float2 gamma[N], beta[N];
-    each_channel<N, V>(s, r, p, [&](int j, int channel) {
-        put(gamma, j, p.active && gammas ? NormIo<IO>::one(gammas, channel) : 1.0f);
-        put(beta, j, p.active && betas ? NormIo<IO>::one(betas, channel) : 0.0f);
-    });
+    Runs<N, P> gamma, beta;
+    parameters(s, r, p, gammas, betas, &gamma, &beta);
     const int group = r.width(p.column * V);                  // of the block, that of the first element
-    const unsigned steps = group_steps<N, V>(s, p.column * V - group * s.width);
+    const unsigned steps = group_steps<Runs<N, P>>(s, p.column * V - group * s.width);
     const int each = s.C / s.groups, channels = p.groups * each, row = p.columns * r.sums;
     float2* sums = m.side + blockDim.x * r.sums;              // a channel's, of this instance and of all so far
     float2* total = sums + r.groups * each;
@@ -344,28 +323,28 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
     int round = 0;
     for (int64_t b = p.b; b < s.B; b += r.instances, ++round) {
         // z = (x - mean) * (rstd * gamma) + beta;  rstd comes to the sums of dz * (x - mean) at the end
-        float2 mean[N], scale[N], rstd[N];
-        each_group<N, V>(steps, stats + b * s.groups + p.first_group + group, [&](int j, float2 v) {
-            put(mean, j, v.x);
-            put(rstd, j, v.y);
+        Runs<N, P> mean, scale, rstd;
+        each_group<Runs<N, P>>(steps, stats + b * s.groups + p.first_group + group, [&](int e, float2 v) {
+            mean.set(e, v.x);
+            rstd.set(e, v.y);
         });
 #pragma unroll
-        for (int j = 0; j < N; ++j) scale[j] = mul2(rstd[j], gamma[j]);
+        for (int j = 0; j < N; ++j) scale.v[j] = mul2(rstd.v[j], gamma.v[j]);
         float2 db[P] = {}, dg[P] = {}, xc[P], dz[P];
         auto both = [&](int i) {
             NormIo<IO>::widen(slot[i * pitch], xc);
             NormIo<IO>::widen(slot[i * pitch + second], dz);
 #pragma unroll
             for (int j = 0; j < P; ++j) {
-                xc[j] = sub2(xc[j], of_pair(mean, j));
-                if (ACT != EQL_ACT_NONE) dz[j] = mul2(dz[j], slope<ACT>(fma2(xc[j], of_pair(scale, j), of_pair(beta, j))));
+                xc[j] = sub2(xc[j], mean.of(j));
+                if (ACT != EQL_ACT_NONE) dz[j] = mul2(dz[j], slope<ACT>(fma2(xc[j], scale.of(j), beta.of(j))));
             }
         };
         auto add = [&](int i) {
             both(i);
 #pragma unroll
             for (int j = 0; j < P; ++j) {
-                const int k = N == 1 ? j % 2 : j;             // (two chains are enough where one number comes out)
+                const int k = N == 1 ? j % 2 : j * N / P;     // (two chains are enough where one number comes out)
                 db[k] = add2(db[k], dz[j]);
                 dg[k] = fma2(dz[j], xc[j], dg[k]);
             }
@@ -379,19 +358,18 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
         // The thread's sums side by side: r.sums of them, of r.run neighbouring elements each (a channel's).
         if (N == 1) {
             db[0] = add2(db[0], db[1]);
-            dg[0] = mul2(add2(dg[0], dg[1]), rstd[0]);
+            dg[0] = mul2(add2(dg[0], dg[1]), rstd.v[0]);
             m.side[threadIdx.x] = make_float2(db[0].x + db[0].y, dg[0].x + dg[0].y);
         } else {
-            float2 run = make_float2(0.0f, 0.0f);
 #pragma unroll
-            for (int j = 0; j < P; ++j) dg[j] = mul2(dg[j], of_pair(rstd, j));
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                run.x += element(db, j);
-                run.y += element(dg, j);
-                if ((j + 1) % r.run == 0) {
-                    m.side[threadIdx.x * r.sums + j / r.run] = run;
-                    run = make_float2(0.0f, 0.0f);
+            for (int j = 0; j < N; ++j) {
+                dg[j] = mul2(dg[j], rstd.v[j]);
+                float2* to = m.side + threadIdx.x * r.sums;
+                if (r.sums <= N) {
+                    to[j] = make_float2(db[j].x + db[j].y, dg[j].x + dg[j].y);
+                } else {                                      // (each half of a pair is a channel's)
+                    to[2 * j] = make_float2(db[j].x, dg[j].x);
+                    to[2 * j + 1] = make_float2(db[j].y, dg[j].y);
                 }
             }
         }
@@ -444,15 +422,15 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
             __syncthreads();
         }
         // dx = dz * (rstd * gamma) - (x - mean) * (rstd * rstd * second) - rstd * first
-        float2 off1[N], off2[N];
-        each_group<N, V>(steps, m.result + group, [&](int j, float2 v) {
-            put(off1, j, -v.x);
-            put(off2, j, -v.y);
+        Runs<N, P> off1, off2;
+        each_group<Runs<N, P>>(steps, m.result + group, [&](int e, float2 v) {
+            off1.set(e, -v.x);
+            off2.set(e, -v.y);
         });
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            off1[j] = mul2(off1[j], rstd[j]);
-            off2[j] = mul2(mul2(off2[j], rstd[j]), rstd[j]);
+            off1.v[j] = mul2(off1.v[j], rstd.v[j]);
+            off2.v[j] = mul2(mul2(off2.v[j], rstd.v[j]), rstd.v[j]);
         }
         const Rows next = lengths || b + r.instances >= s.B ? Rows(s, r, p, lengths, b + r.instances) : rows;
         const int count_next = p.active ? next.of(p.lane) : 0;
@@ -462,7 +440,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
             both(i);
             float2 f[P];
 #pragma unroll
-            for (int j = 0; j < P; ++j) f[j] = fma2(xc[j], of_pair(off2, j), fma2(dz[j], of_pair(scale, j), of_pair(off1, j)));
+            for (int j = 0; j < P; ++j) f[j] = fma2(xc[j], off2.of(j), fma2(dz[j], scale.of(j), off1.of(j)));
             *to = NormIo<IO>::narrow(f);
             to += step;
         };
@@ -484,7 +462,8 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
 
 constexpr int kFewThreads = 256, kManyForward = 1024, kManyBackward = 512;
 // CTAs of 256 threads to an SM, by the registers that the kernels then may use.
-constexpr int kForwardCtas = 4, kGradientCtasTuple = 3, kGradientCtas = 2;
+constexpr int forward_ctas(int n, int P) { return n < P ? 4 : 3; }
+constexpr int gradient_ctas(int n, int P) { return n < P ? 3 : 2; }
 
 ResidentNorm resident_norm_plan(const NormShape& s, eql_dtype_t dtype, bool backward) {
     ResidentNorm r{};
@@ -502,7 +481,7 @@ ResidentNorm resident_norm_plan(const NormShape& s, eql_dtype_t dtype, bool back
     if (columns > (backward ? kManyBackward : kManyForward)) return r;
     r.threads = columns <= kFewThreads ? kFewThreads : backward ? kManyBackward : kManyForward;
     r.blocks = (s.groups + r.groups - 1) / r.groups;
-    r.run = s.T % V == 0 ? V : V % s.T == 0 ? s.T : 1;
+    r.run = run_length(s.T, V);
     r.sums = V / r.run;
     r.tuple = Divisor(s.T);
     r.width = Divisor(s.width);
@@ -531,7 +510,7 @@ ResidentNorm resident_norm_plan(const NormShape& s, eql_dtype_t dtype, bool back
     while (r.share < 32 && r.share * 2 * channels <= r.threads) r.share *= 2;
     // One CTA after the other takes a block's instances, as many side by side as are resident together, and all about the same number.
     // (A cluster takes one: how many of them are resident depends on the SMs that the device has in each of its parts.)
-    int64_t together = 228 * 1024 / (r.shared_bytes + 1024), most = backward ? (s.T % V == 0 ? kGradientCtasTuple : kGradientCtas) : kForwardCtas;
+    int64_t together = 228 * 1024 / (r.shared_bytes + 1024), most = backward ? gradient_ctas(runs_of(s.T, V), V / 2) : forward_ctas(runs_of(s.T, V), V / 2);
     if (r.threads != kFewThreads) most = 1;
     if (together > most) together = most;
     together = together * kNumSMs / (r.blocks * r.cluster);
@@ -567,13 +546,14 @@ cudaError_t launch_resident_norm(const NormShape& s, const ResidentNorm& r, eql_
         constexpr int V = NormIo<IO>::kVec, P = V / 2;
         return dispatch_act(s.act, [&](auto act) {
             constexpr int ACT = decltype(act)::value;
-            static SmemLimitOnce limits[3];
+            static SmemLimitOnce limits[4];
             auto launch = [&](auto kernel, SmemLimitOnce& limit) {
                 return launch_resident(kernel, limit, s, r, stream, (const uint4*)x, (const IO*)gamma, (const IO*)beta, lengths, (uint4*)y, (float2*)stats);
             };
             if (r.threads != kFewThreads) return launch(resident_norm_kernel<IO, ACT, P, kManyForward, 1>, limits[0]);
-            return s.T % V == 0 ? launch(resident_norm_kernel<IO, ACT, 1, kFewThreads, kForwardCtas>, limits[1])
-                                : launch(resident_norm_kernel<IO, ACT, P, kFewThreads, kForwardCtas>, limits[2]);
+            if (runs_of(s.T, V) == 1) return launch(resident_norm_kernel<IO, ACT, 1, kFewThreads, forward_ctas(1, P)>, limits[1]);
+            if (runs_of(s.T, V) < P) return launch(resident_norm_kernel<IO, ACT, 2, kFewThreads, forward_ctas(2, P)>, limits[2]);
+            return launch(resident_norm_kernel<IO, ACT, P, kFewThreads, forward_ctas(P, P)>, limits[3]);
         });
     });
 }
@@ -585,14 +565,15 @@ cudaError_t launch_resident_gradient(const NormShape& s, const ResidentNorm& r, 
         constexpr int V = NormIo<IO>::kVec, P = V / 2;
         return dispatch_act(s.act, [&](auto act) {
             constexpr int ACT = decltype(act)::value;
-            static SmemLimitOnce limits[3];
+            static SmemLimitOnce limits[4];
             auto launch = [&](auto kernel, SmemLimitOnce& limit) {
                 return launch_resident(kernel, limit, s, r, stream, (const uint4*)x, (const uint4*)dy, (const IO*)gamma, (const IO*)beta, lengths,
                                        (const float2*)stats, (uint4*)dx, (float2*)parts);
             };
             if (r.threads != kFewThreads) return launch(resident_gradient_kernel<IO, ACT, P, kManyBackward, 1>, limits[0]);
-            return s.T % V == 0 ? launch(resident_gradient_kernel<IO, ACT, 1, kFewThreads, kGradientCtasTuple>, limits[1])
-                                : launch(resident_gradient_kernel<IO, ACT, P, kFewThreads, kGradientCtas>, limits[2]);
+            if (runs_of(s.T, V) == 1) return launch(resident_gradient_kernel<IO, ACT, 1, kFewThreads, gradient_ctas(1, P)>, limits[1]);
+            if (runs_of(s.T, V) < P) return launch(resident_gradient_kernel<IO, ACT, 2, kFewThreads, gradient_ctas(2, P)>, limits[2]);
+            return launch(resident_gradient_kernel<IO, ACT, P, kFewThreads, gradient_ctas(P, P)>, limits[3]);
         });
     });
 }

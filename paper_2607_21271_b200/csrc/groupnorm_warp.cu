@@ -267,7 +267,7 @@ WarpNorm warp_norm_plan(const NormShape& s, eql_dtype_t dtype, bool backward) {
     w.groups = s.groups < chairs ? s.groups : chairs;
     w.instances = chairs / w.groups;
     w.group_blocks = (s.groups + w.groups - 1) / w.groups;
-    w.sums = s.T % V == 0 ? 1 : V % s.T == 0 ? V / s.T : V;
+    w.sums = V / run_length(s.T, V);
     w.shared_bytes = backward ? w.groups * w.instances * w.unit * w.sums * 8 : 0;
     // CTAs that are resident together walk over the instances, all about the same number
     const int together = kNumSMs * (backward ? gradient_ctas(w.each, w.sums) : forward_ctas(w.each, w.sums == 1));
