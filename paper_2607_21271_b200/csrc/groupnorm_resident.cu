@@ -89,16 +89,19 @@ template <typename Use, typename Copy>
 __device__ __forceinline__ void refill(int mine, int count, Use&& use, Copy&& copy) {
     const int half = (count + 1) / 2;
     int i = 0;
+#pragma unroll 2
     for (; i < half; ++i) {
         if (i < mine) use(i);
         copy(i);
     }
     copies_commit();
+#pragma unroll 2
     for (; i < count; ++i) {
         if (i < mine) use(i);
         copy(i);
     }
     copies_commit();
+#pragma unroll 2
     for (; i < mine; ++i) use(i);
 }
 
@@ -190,30 +193,40 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_norm_kernel(NormShape 
         };
         const int half = (mine + 1) / 2;
         copies_wait<1>();
+#pragma unroll 2
         for (int i = 0; i < half; ++i) add(i);
         copies_wait<0>();
+#pragma unroll 2
         for (int i = half; i < mine; ++i) add(i);
-        if (whole) {                                          // the columns of a vector have as many values each
-            float2 sum = moments.mean[0], squares = moments.m2[0];
+        // The columns of `pairs` pairs from `first` on, which have as many values each.
+        auto together = [&](int first, int pairs) {
+            float2 sum = moments.mean[first], squares = moments.m2[first];
 #pragma unroll
-            for (int j = 1; j < P; ++j) sum = add2(sum, moments.mean[j]);
-            const float mean = (sum.x + sum.y) * (1.0f / V);
-            float2 off = sub2(moments.mean[0], pair(mean)), around = mul2(off, off);
+            for (int j = 1; j < pairs; ++j) sum = add2(sum, moments.mean[first + j]);
+            const float mean = (sum.x + sum.y) * (0.5f / pairs);
+            float2 off = sub2(moments.mean[first], pair(mean)), around = mul2(off, off);
 #pragma unroll
-            for (int j = 1; j < P; ++j) {
-                off = sub2(moments.mean[j], pair(mean));
+            for (int j = 1; j < pairs; ++j) {
+                off = sub2(moments.mean[first + j], pair(mean));
                 around = fma2(off, off, around);
-                squares = add2(squares, moments.m2[j]);
+                squares = add2(squares, moments.m2[first + j]);
             }
             squares = fma2(around, pair(moments.rows), squares);
-            const float m2 = squares.x + squares.y;
+            return make_float2(mean, squares.x + squares.y);
+        };
+        if (whole) {
+            const float2 t = together(0, P);
+            const float mean = t.x, m2 = t.y;
             if (p.groups == 1) {                              // every thread's: a warp's together
                 const float n = moments.rows * V, all = warp_sum(n), middle = all > 0.0f ? __fdividef(warp_sum(n * mean), all) : 0.0f;
                 const float around_all = warp_sum(fmaf(n * (mean - middle), mean - middle, m2));
                 if ((threadIdx.x & 31) == 0) { m.side[2 * warp] = make_float2(middle, around_all); m.side[2 * warp + 1].x = all; }
             } else {
-                m.side[threadIdx.x] = make_float2(mean, m2);
+                m.side[threadIdx.x] = t;
             }
+        } else if (N == 2 && P > 2) {
+            m.side[threadIdx.x * 2] = together(0, P / 2);
+            m.side[threadIdx.x * 2 + 1] = together(P / 2, P / 2);
         } else {
 #pragma unroll
             for (int j = 0; j < V; ++j) m.side[threadIdx.x * V + j] = make_float2(element(moments.mean, j), element(moments.m2, j));
@@ -226,8 +239,8 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_norm_kernel(NormShape 
             if (whole && p.groups == 1) {
                 t = moments_of(count, warps, [&](int e, float* n) { *n = m.side[2 * e + 1].x; return m.side[2 * e]; });
             } else {
-                // entries of a lane of rows: the group's vectors, or where they cross its border its elements
-                const int per = whole ? 1 : V, row = p.columns * per;
+                // entries of a lane of rows: the group's vectors, or where they cross its border its runs
+                const int per = whole ? 1 : Runs<N, P>::kEntries, row = p.columns * per;
                 const float more = (float)((rows.each + 1) * (V / per)), fewer = (float)(rows.each * (V / per));
                 t = moments_of(count, min(p.lanes, rows.all) * (int)r.entry.d, [&](int e, float* n) {
                     const int l = r.entry(e);
@@ -331,17 +344,20 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
 #pragma unroll
         for (int j = 0; j < N; ++j) scale.v[j] = mul2(rstd.v[j], gamma.v[j]);
         float2 db[P] = {}, dg[P] = {}, xc[P], dz[P];
-        auto both = [&](int i) {
+        // A float dz takes the place of dy, and is there the second time; in 16 bits it would lose, and is computed again.
+        constexpr bool kKeep = sizeof(IO) == 4 && ACT != EQL_ACT_NONE;
+        auto both = [&](int i, bool again) {
             NormIo<IO>::widen(slot[i * pitch], xc);
             NormIo<IO>::widen(slot[i * pitch + second], dz);
 #pragma unroll
             for (int j = 0; j < P; ++j) {
                 xc[j] = sub2(xc[j], mean.of(j));
-                if (ACT != EQL_ACT_NONE) dz[j] = mul2(dz[j], slope<ACT>(fma2(xc[j], scale.of(j), beta.of(j))));
+                if (ACT != EQL_ACT_NONE && !(kKeep && again)) dz[j] = mul2(dz[j], slope<ACT>(fma2(xc[j], scale.of(j), beta.of(j))));
             }
         };
         auto add = [&](int i) {
-            both(i);
+            both(i, false);
+            if (kKeep) slot[i * pitch + second] = NormIo<IO>::narrow(dz);
 #pragma unroll
             for (int j = 0; j < P; ++j) {
                 const int k = N == 1 ? j % 2 : j * N / P;     // (two chains are enough where one number comes out)
@@ -351,8 +367,10 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
         };
         const int half = (mine + 1) / 2;
         copies_wait<1>();
+#pragma unroll 2
         for (int i = 0; i < half; ++i) add(i);
         copies_wait<0>();
+#pragma unroll 2
         for (int i = half; i < mine; ++i) add(i);
 
         // The thread's sums side by side: r.sums of them, of r.run neighbouring elements each (a channel's).
@@ -437,7 +455,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
         uint4* to = dx + p.at(s, b);
         const uint4 *from_x = x + p.at(s, b + r.instances), *from_dy = dy + p.at(s, b + r.instances);
         auto apply = [&](int i) {
-            both(i);
+            both(i, true);
             float2 f[P];
 #pragma unroll
             for (int j = 0; j < P; ++j) f[j] = fma2(xc[j], off2.of(j), fma2(dz[j], scale.of(j), off1.of(j)));
@@ -461,9 +479,10 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
 }  // namespace
 
 constexpr int kFewThreads = 256, kManyForward = 1024, kManyBackward = 512;
-// CTAs of 256 threads to an SM, by the registers that the kernels then may use.
+// CTAs of 256 threads to an SM, by the registers that the kernels then may use.  (Backward, with two instead of three and two rows of a
+// thread side by side: 128 x 3136 x 384 bfloat16, forward and backward, 533 -> 519 us.)
 constexpr int forward_ctas(int n, int P) { return n < P ? 4 : 3; }
-constexpr int gradient_ctas(int n, int P) { return n < P ? 3 : 2; }
+constexpr int kGradientCtas = 2;
 
 ResidentNorm resident_norm_plan(const NormShape& s, eql_dtype_t dtype, bool backward) {
     ResidentNorm r{};
@@ -485,10 +504,11 @@ ResidentNorm resident_norm_plan(const NormShape& s, eql_dtype_t dtype, bool back
     r.sums = V / r.run;
     r.tuple = Divisor(s.T);
     r.width = Divisor(s.width);
-    r.entry = Divisor(s.width % V == 0 ? s.width / V : s.width);
+    const int per = s.width % V == 0 ? 1 : runs_of(s.T, V) < V / 2 ? runs_of(s.T, V) : V;      // entries of a vector
+    r.entry = Divisor(s.width * per / V);
     r.runs = Divisor(s.T / r.run);
     const int channels = r.groups * (s.C / s.groups), lanes = (int)(r.threads / columns);
-    const int side = backward ? r.threads * r.sums + 2 * channels : s.width % V == 0 ? r.threads : r.threads * V;
+    const int side = backward ? r.threads * r.sums + 2 * channels : r.threads * per;
     for (r.cluster = 1; r.cluster <= kMaxCluster; r.cluster *= 2) {
         r.rows = (s.S + r.cluster - 1) / r.cluster;
         const int64_t slots = (r.rows + lanes - 1) / lanes, slot_bytes = slots * r.threads * 16 * (backward ? 2 : 1);
@@ -510,7 +530,7 @@ ResidentNorm resident_norm_plan(const NormShape& s, eql_dtype_t dtype, bool back
     while (r.share < 32 && r.share * 2 * channels <= r.threads) r.share *= 2;
     // One CTA after the other takes a block's instances, as many side by side as are resident together, and all about the same number.
     // (A cluster takes one: how many of them are resident depends on the SMs that the device has in each of its parts.)
-    int64_t together = 228 * 1024 / (r.shared_bytes + 1024), most = backward ? gradient_ctas(runs_of(s.T, V), V / 2) : forward_ctas(runs_of(s.T, V), V / 2);
+    int64_t together = 228 * 1024 / (r.shared_bytes + 1024), most = backward ? kGradientCtas : forward_ctas(runs_of(s.T, V), V / 2);
     if (r.threads != kFewThreads) most = 1;
     if (together > most) together = most;
     together = together * kNumSMs / (r.blocks * r.cluster);
@@ -571,9 +591,9 @@ cudaError_t launch_resident_gradient(const NormShape& s, const ResidentNorm& r, 
                                        (const float2*)stats, (uint4*)dx, (float2*)parts);
             };
             if (r.threads != kFewThreads) return launch(resident_gradient_kernel<IO, ACT, P, kManyBackward, 1>, limits[0]);
-            if (runs_of(s.T, V) == 1) return launch(resident_gradient_kernel<IO, ACT, 1, kFewThreads, gradient_ctas(1, P)>, limits[1]);
-            if (runs_of(s.T, V) < P) return launch(resident_gradient_kernel<IO, ACT, 2, kFewThreads, gradient_ctas(2, P)>, limits[2]);
-            return launch(resident_gradient_kernel<IO, ACT, P, kFewThreads, gradient_ctas(P, P)>, limits[3]);
+            if (runs_of(s.T, V) == 1) return launch(resident_gradient_kernel<IO, ACT, 1, kFewThreads, kGradientCtas>, limits[1]);
+            if (runs_of(s.T, V) < P) return launch(resident_gradient_kernel<IO, ACT, 2, kFewThreads, kGradientCtas>, limits[2]);
+            return launch(resident_gradient_kernel<IO, ACT, P, kFewThreads, kGradientCtas>, limits[3]);
         });
     });
 }
