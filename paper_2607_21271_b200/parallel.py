@@ -50,7 +50,7 @@ def allreduce_weight_grads(dw, db=None, group=None, flat=None, async_op=False):
     return None
 
 
-def dp_training_step(fwd, weight_grad, data_grad, flat, group=None, side_stream=None, mark=None):
+def dp_training_step(fwd, weight_grad, data_grad, flat, group=None, side_stream=None, mark=None, update=None):
     """One data-parallel training step of the layer, in the order that hides its one exchange step.
 
     forward -> weight gradient -> START the all-reduce of the flat dw|db buffer -> data gradient -> wait for the
@@ -61,6 +61,8 @@ def dp_training_step(fwd, weight_grad, data_grad, flat, group=None, side_stream=
     weight gradient, so that it overlaps the data-gradient kernel, and the current stream waits for it at the end.
     `mark(i)`, if given, is called at the phase boundaries (0: start, 1: after fwd, 2: after the weight gradient and the
     start of the exchange, 3: after the data gradient) so that a caller can record timing events.
+    `update`, if given, is called last, when the summed gradients are in place (on CUDA: enqueued behind them): what turns them
+    into the next parameters on every rank alike, e.g. eqlinear_adamw_clip, eqlinear_adamw_step and eqlinear_plan_set_weight.
     Returns the list of phase names in the order they ran."""
     import torch
 
@@ -92,4 +94,7 @@ def dp_training_step(fwd, weight_grad, data_grad, flat, group=None, side_stream=
     if work is not None:
         work.wait()                     # CUDA: the current stream waits for the collective; CPU: blocks until it is done
     order.append("allreduce_done")
+    if update is not None:
+        update()
+        order.append("update")
     return order
