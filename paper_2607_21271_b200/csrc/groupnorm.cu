@@ -15,6 +15,8 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kUnroll = 4;    // vectors a thread has on their way
+// CTAs resident together, by the registers that the kernels then may use.
+constexpr int range_ctas(int n, int P) { return n < P ? 4 : 2; }
 
 // Row ranges and pieces of an instance.
 struct Ranges {
@@ -76,7 +78,7 @@ __device__ __forceinline__ void walk(int count, Load&& load, Use&& use) {
 }
 
 template <typename IO>
-__global__ void __launch_bounds__(kThreads) part_moments_kernel(NormShape s, Ranges g, const uint4* x, const int32_t* lengths) {
+__global__ void __launch_bounds__(kThreads, 4) part_moments_kernel(NormShape s, Ranges g, const uint4* x, const int32_t* lengths) {
     constexpr int V = NormIo<IO>::kVec;
     ptx::grid_handover();
     __shared__ float2 shared[kThreads * V];
@@ -182,7 +184,7 @@ struct Column {
 };
 
 template <typename IO, int ACT, int N>
-__global__ void __launch_bounds__(kThreads) apply_kernel(NormShape s, Ranges g, const uint4* x, const IO* gamma, const IO* beta,
+__global__ void __launch_bounds__(kThreads, range_ctas(N, NormIo<IO>::kVec / 2)) apply_kernel(NormShape s, Ranges g, const uint4* x, const IO* gamma, const IO* beta,
                                                          const int32_t* lengths, uint4* y) {
     constexpr int V = NormIo<IO>::kVec;
     ptx::grid_handover();
@@ -201,7 +203,7 @@ __global__ void __launch_bounds__(kThreads) apply_kernel(NormShape s, Ranges g, 
 }
 
 template <typename IO, int ACT, int N>
-__global__ void __launch_bounds__(kThreads) part_sums_kernel(NormShape s, Ranges g, const uint4* x, const uint4* dy, const IO* gamma, const IO* beta,
+__global__ void __launch_bounds__(kThreads, range_ctas(N, NormIo<IO>::kVec / 2)) part_sums_kernel(NormShape s, Ranges g, const uint4* x, const uint4* dy, const IO* gamma, const IO* beta,
                                                              const int32_t* lengths, const float* stats) {
     constexpr int V = NormIo<IO>::kVec;
     ptx::grid_handover();
@@ -300,7 +302,7 @@ __global__ void __launch_bounds__(kThreads) group_sums_kernel(NormShape s, Range
 }
 
 template <typename IO, int ACT, int N>
-__global__ void __launch_bounds__(kThreads) apply_gradient_kernel(NormShape s, Ranges g, const uint4* x, const uint4* dy, const IO* gamma, const IO* beta,
+__global__ void __launch_bounds__(kThreads, range_ctas(N, NormIo<IO>::kVec / 2)) apply_gradient_kernel(NormShape s, Ranges g, const uint4* x, const uint4* dy, const IO* gamma, const IO* beta,
                                                                   const int32_t* lengths, const float* stats, uint4* dx) {
     constexpr int V = NormIo<IO>::kVec;
     ptx::grid_handover();
@@ -366,12 +368,13 @@ eql_status_t check_norm(const eql_groupnorm_t* n, NormShape* s) {
     return EQL_OK;
 }
 
-// Ranges of rows so that a launch fills the device a few times over, of 32 rows at least.
+// Ranges of rows so that a launch fills the device once, of 32 rows at least.  (One map of 65536 x 1024 half precision, forward and
+// backward: one filling 228 us, two 240.)
 Ranges range_plan(const NormShape& s, eql_dtype_t dtype, bool backward, char* scratch, size_t* bytes) {
     Ranges g{};
     const int V = dtype == EQL_FP32 ? 4 : 8;
     g.pieces = (s.vectors + kThreads - 1) / kThreads;
-    const int64_t wanted = (8 * kNumSMs + s.B * g.pieces - 1) / (s.B * g.pieces);
+    const int64_t wanted = 4 * kNumSMs / (s.B * g.pieces) > 0 ? 4 * kNumSMs / (s.B * g.pieces) : 1;
     const int64_t most = s.S / 32 > 1 ? s.S / 32 : 1;
     const int64_t ranges = wanted < most ? wanted : most;
     g.rows = (s.S + ranges - 1) / ranges;
