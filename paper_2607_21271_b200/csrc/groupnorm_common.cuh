@@ -211,15 +211,16 @@ __device__ __forceinline__ float2 sigmoid(float2 z) {
     return reciprocal(add2(exp2_fast(mul2(z, pair(-1.44269504088896341f))), pair(1.0f)));
 }
 // Phi(-|z|) = erfc(|z| / sqrt 2) / 2 by the rational approximation 7.1.26 of Abramowitz and Stegun (error of erfc at most 1.5e-7, a float's
-// at 1; falling with exp(-z^2 / 2) in the tail).  `density`: exp(-z^2 / 2).
+// at 1; falling with exp(-z^2 / 2) in the tail).  `density`: phi(z) = exp(-z^2 / 2) / sqrt(2 pi), its constant part of the exponent, and
+// the polynomial's coefficients (halves of theirs) divided by it.
 __device__ __forceinline__ float2 tail_of_normal(float2 z, float2* density) {
-    const float2 n = minus_abs(z);
-    const float2 t = reciprocal(fma2(n, pair(-0.3275911f * 0.70710678118654752f), pair(1.0f)));
-    *density = exp2_fast(mul2(mul2(z, z), pair(-0.72134752044448170f)));
-    float2 p = fma2(t, pair(0.5f * 1.061405429f), pair(0.5f * -1.453152027f));
-    p = fma2(p, t, pair(0.5f * 1.421413741f));
-    p = fma2(p, t, pair(0.5f * -0.284496736f));
-    p = fma2(p, t, pair(0.5f * 0.254829592f));
+    constexpr float kPerDensity = 0.5f * 2.50662827463100050242f;
+    const float2 t = reciprocal(fma2(minus_abs(z), pair(-0.3275911f * 0.70710678118654752f), pair(1.0f)));
+    *density = exp2_fast(fma2(mul2(z, z), pair(-0.72134752044448170f), pair(-1.32574806473615915f)));
+    float2 p = fma2(t, pair(kPerDensity * 1.061405429f), pair(kPerDensity * -1.453152027f));
+    p = fma2(p, t, pair(kPerDensity * 1.421413741f));
+    p = fma2(p, t, pair(kPerDensity * -0.284496736f));
+    p = fma2(p, t, pair(kPerDensity * 0.254829592f));
     return mul2(mul2(p, t), *density);
 }
 
@@ -237,7 +238,7 @@ template <int ACT> __device__ __forceinline__ float2 slope(float2 z) {
         float2 density;
         const float2 h = sub2(pair(0.5f), tail_of_normal(z, &density));
         const float2 cdf = add2(make_float2(copysignf(h.x, z.x), copysignf(h.y, z.y)), pair(0.5f));
-        return fma2(mul2(z, pair(0.39894228040143267794f)), density, cdf);
+        return fma2(z, density, cdf);
     }
     if (ACT == EQL_ACT_SILU) {
         const float2 p = sigmoid(z);
