@@ -319,7 +319,8 @@ eql_status_t eqlinear_step_host(eqlinear_plan_t plan, const void* x_host, const 
  *     xh = (x - mean) * rstd     z = gamma[c] * xh + beta[c]     y = act(z)
  *
  * S = 1 is the norm of every token by itself (groups = 1: layer norm); T = 1 the ordinary group norm.  Statistics,
- * sums and everything between input and output are float; y and dx are rounded once. */
+ * sums and everything between input and output are float; y and dx are rounded once.  There is no plan: a call belongs to the
+ * current device, whose memory all its pointers are, and calls that overlap in time need scratch of their own. */
 typedef enum { EQL_ACT_NONE = 0, EQL_ACT_GELU = 1 /* z * Phi(z), exact form */, EQL_ACT_SILU = 2 /* z / (1 + exp(-z)) */ } eql_act_t;
 
 typedef struct {
@@ -348,7 +349,7 @@ eql_status_t eqlinear_groupnorm_fwd(const eql_groupnorm_t* norm, const void* x, 
  *     dbeta[c] = sum of dz,  dgamma[c] = sum of dz * xh,  over instances, positions and tuple
  *     dx = rstd * (gamma * dz - (s1 + xh * s2) / (n_b * C / groups * T)),  s1, s2: sums of gamma * dz and gamma * dz * xh over the group
  *   dx              device [B, S, C*T]; rows of padding are left as they are
- *   dgamma, dbeta   device float [C], overwritten; either may be NULL
+ *   dgamma, dbeta   device float [C], overwritten (zeros where there are no rows at all); either may be NULL
  * Sums run in a fixed order: results are the same bits from run to run. */
 eql_status_t eqlinear_groupnorm_bwd(const eql_groupnorm_t* norm, const void* x, const void* dy, const void* gamma, const void* beta,
                                     const int32_t* lengths, const float* stats, void* dx, void* dgamma, void* dbeta,
@@ -370,7 +371,11 @@ eql_status_t eqlinear_groupnorm_bwd(const eql_groupnorm_t* norm, const void* x, 
  * one for v: m is held as e4m3 codes of m * (448 / max|m|) with scale max|m| / 448, v as e5m2 codes of v * (57344 / max v)
  * with scale max v / 57344, both rounded to nearest even; a v above zero never becomes code zero (the least code, 2^-16,
  * stands for it), so that a later step does not divide by nothing.  A v below 2^-126 counts as zero in the denominator.  A block whose largest magnitude is below 2^-100 is held
- * as zeros.  The step itself uses the states before they are rounded.  Zeroed codes and scales are valid initial states. */
+ * as zeros.  The step itself uses the states before they are rounded.  Zeroed codes and scales are valid initial states.
+ *
+ * As a plan, an optimiser may be used from one stream at a time, and only while the device that it was built on is current
+ * (EQL_ERR_INVALID_ARG otherwise).  Without eqlinear_adamw_clip in front, gradients that are not finite go into parameters and
+ * states. */
 typedef struct eqlinear_adamw_s* eqlinear_adamw_t;   /* opaque host object */
 
 typedef struct {
@@ -400,7 +405,7 @@ eql_status_t eqlinear_adamw_workspace_bytes(const eql_adamw_tensor_t* tensors, i
 /* Build an optimiser on the current device over `count` tensors (host array, copied).  Its table of tensors and its step
  * counter (0) live in `workspace` (device, 256-byte aligned, the caller's, untouched until eqlinear_adamw_destroy).  No two
  * of the buffers that a step writes may share bytes, nor may one share bytes with a gradient or the workspace
- * (EQL_ERR_INVALID_ARG).  The table travels over `stream`, which is synchronised: not during stream capture
+ * (EQL_ERR_INVALID_ARG); nor may one be memory of the host or of another device.  The table travels over `stream`, which is synchronised: not during stream capture
  * (EQL_ERR_INVALID_ARG).  On error *opt is set to NULL. */
 eql_status_t eqlinear_adamw(eqlinear_adamw_t* opt, const eql_adamw_tensor_t* tensors, int count, int state_bits,
                             void* workspace, size_t workspace_bytes, void* stream);

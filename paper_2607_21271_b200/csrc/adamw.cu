@@ -548,6 +548,18 @@ eql_status_t check_tensor(const eql_adamw_tensor_t& t, int state_bits, Range* ra
     return EQL_OK;
 }
 
+// Whether all of a tensor's buffers are memory of `device`: a kernel that met another pointer would fault.
+bool on_device(const eql_adamw_tensor_t& t, int device) {
+    const void* pointers[] = {t.param, t.master, t.grad, t.exp_avg, t.exp_avg_sq, t.exp_avg_scale, t.exp_avg_sq_scale};
+    for (const void* p : pointers) {
+        if (!p) continue;
+        cudaPointerAttributes a{};
+        if (cudaPointerGetAttributes(&a, p) != cudaSuccess) { cudaGetLastError(); return false; }
+        if (a.type != cudaMemoryTypeManaged && (a.type != cudaMemoryTypeDevice || a.device != device)) return false;
+    }
+    return true;
+}
+
 // Whether a written range shares bytes with any other.
 bool ranges_clash(Range* ranges, int n) {
     std::sort(ranges, ranges + n, [](const Range& a, const Range& b) { return a.begin < b.begin; });
@@ -630,6 +642,8 @@ eql_status_t eqlinear_adamw(eqlinear_adamw_t* opt, const eql_adamw_tensor_t* ten
     if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) return EQL_ERR_CUDA;
     if (major != 10) return EQL_ERR_ARCH;
     if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return EQL_ERR_CUDA;
+    for (int i = 0; i < count; ++i)
+        if (tensors[i].numel > 0 && !on_device(tensors[i], dev)) return EQL_ERR_INVALID_ARG;
     const cudaStream_t s = (cudaStream_t)stream;
     cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
     if (cudaStreamIsCapturing(s, &capturing) != cudaSuccess) return EQL_ERR_CUDA;

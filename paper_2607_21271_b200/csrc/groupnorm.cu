@@ -519,6 +519,7 @@ eql_status_t eqlinear_groupnorm_bwd(const eql_groupnorm_t* norm, const void* x, 
     NormShape s;
     if (eql_status_t st = check_norm(norm, &s); st != EQL_OK) return st;
     if (!aligned(dgamma, 16) || !aligned(dbeta, 16)) return EQL_ERR_ALIGNMENT;
+    if (dgamma && dbeta && overlap(dgamma, s.C * sizeof(float), dbeta, s.C * sizeof(float))) return EQL_ERR_INVALID_ARG;
     const cudaStream_t st = (cudaStream_t)stream;
     if (s.B == 0 || s.S == 0) {
         if (dgamma && cudaMemsetAsync(dgamma, 0, s.C * sizeof(float), st) != cudaSuccess) return EQL_ERR_CUDA;

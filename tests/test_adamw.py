@@ -450,3 +450,17 @@ def test_tensors_of_different_types_and_none_with_elements():
         assert float(norm) == 0.0 and eq.eqlinear_adamw_info(o.h, o.stream).step == 1
     finally:
         o.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("which", ["param", "master", "grad", "exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale"])
+def test_memory_of_the_host_is_refused(which):
+    n = 512
+    args = {k: torch.zeros(n, device="cuda") for k in ("param", "master", "grad", "exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale")}
+    for host in (torch.zeros(n + 16), torch.zeros(n + 16).pin_memory()):
+        at = (-host.data_ptr() % 16) // 4
+        table = [eq.eqlinear_adamw_tensor(**{**args, which: host[at:]}, numel=n, param_dtype=eq.EQL_FP32, grad_dtype=eq.EQL_FP32)]
+        bytes_ = eq.eqlinear_adamw_workspace_bytes(table, 8)
+        workspace = torch.empty(bytes_, dtype=torch.uint8, device="cuda")
+        assert refused(table, 8, workspace, bytes_) == binding.EQL_ERR_INVALID_ARG
+    torch.cuda.synchronize()

@@ -71,7 +71,7 @@ def test_forward_arguments_that_are_refused(change, status):
 @pytest.mark.parametrize("change,status", [
     (dict(x=None), binding.EQL_ERR_INVALID_ARG), (dict(dy=None), binding.EQL_ERR_INVALID_ARG), (dict(dx=None), binding.EQL_ERR_INVALID_ARG),
     (dict(stats=None), binding.EQL_ERR_INVALID_ARG), (dict(dx=1 << 20), binding.EQL_ERR_INVALID_ARG), (dict(dx=2 << 20), binding.EQL_ERR_INVALID_ARG),
-    (dict(dx=(4 << 20) + 8), binding.EQL_ERR_ALIGNMENT), (dict(dgamma=12), binding.EQL_ERR_ALIGNMENT), (dict(dbeta=20), binding.EQL_ERR_ALIGNMENT),
+    (dict(dx=(4 << 20) + 8), binding.EQL_ERR_ALIGNMENT), (dict(dgamma=5 << 20, dbeta=(5 << 20) + 16), binding.EQL_ERR_INVALID_ARG), (dict(dgamma=12), binding.EQL_ERR_ALIGNMENT), (dict(dbeta=20), binding.EQL_ERR_ALIGNMENT),
 ])
 def test_backward_arguments_that_are_refused(change, status):
     assert bwd_status(**change) == status
