@@ -50,6 +50,14 @@ struct Divisor {
     __host__ __device__ explicit Divisor(unsigned by) : d(by), inverse(by > 1 ? 0xffffffffu / by + 1 : 0) {}
     __device__ __forceinline__ unsigned operator()(unsigned e) const { return d > 1 ? __umulhi(e, inverse) : e; }
 };
+// The same for all e and d of 32 bits: ceil(2^64 / d).
+struct WideDivisor {
+    unsigned d;
+    unsigned long long inverse;
+    __host__ __device__ WideDivisor() : d(1), inverse(0) {}
+    __host__ __device__ explicit WideDivisor(unsigned by) : d(by), inverse(by > 1 ? ~0ull / by + 1 : 0) {}
+    __device__ __forceinline__ unsigned operator()(unsigned e) const { return d > 1 ? (unsigned)__umul64hi(e, inverse) : e; }
+};
 struct ResidentNorm {
     bool supported;
     int groups, blocks;       // groups of a block, blocks of a row
@@ -59,6 +67,8 @@ struct ResidentNorm {
     int run, sums, share;     // backward: neighbouring elements summed up in a thread, sums of a vector, lanes that add up a channel
     int slot_bytes, side_offset, shared_bytes;
     Divisor tuple, width, entry, runs;        // T; elements of a group; entries of a group in a row (its vectors, or elements); runs of a tuple
+    Divisor columns, lanes;   // of a full block
+    WideDivisor by_cluster, by_blocks;
 };
 constexpr int kResidentShared = 220 * 1024;
 ResidentNorm resident_norm_plan(const NormShape& s, eql_dtype_t dtype, bool backward);

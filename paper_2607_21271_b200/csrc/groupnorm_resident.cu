@@ -29,19 +29,25 @@ struct Post {
     int first_group, groups;  // of the block
     int vector, column, columns;      // vector of the row; the same within the block, of how many
     int lane, lanes, rank;
+    Divisor by_lanes;
     bool active;
     __device__ __forceinline__ Post(const NormShape& s, const ResidentNorm& r, int V) {
-        const unsigned unit = blockIdx.x / (unsigned)r.cluster, instance = unit / (unsigned)r.blocks, block = unit - instance * r.blocks;
+        const unsigned unit = r.by_cluster(blockIdx.x), instance = r.by_blocks(unit), block = unit - instance * r.blocks;
         rank = blockIdx.x - unit * r.cluster;
         b = instance;
         first_group = block * r.groups;
         groups = min(r.groups, s.groups - first_group);
-        columns = groups * s.width / V;
-        const Divisor by(columns);
-        lanes = by(blockDim.x);
+        Divisor by = r.columns;
+        by_lanes = r.lanes;
+        if (groups < r.groups) {                              // the last block, where it is a narrower one
+            by = Divisor(groups * s.width / V);
+            by_lanes = Divisor(by(blockDim.x));
+        }
+        columns = by.d;
+        lanes = by_lanes.d;
         lane = by(threadIdx.x);
         column = threadIdx.x - lane * columns;
-        vector = first_group * s.width / V + column;
+        vector = first_group * s.width / V + column;          // (V: a power of two)
         active = lane < lanes;
         row0 = (int64_t)rank * r.rows;
     }
@@ -54,7 +60,7 @@ struct Rows {
     __device__ __forceinline__ Rows(const NormShape& s, const ResidentNorm& r, const Post& p, const int32_t* lengths, int64_t b) {
         const int64_t left = b < s.B ? positions_of(lengths, b, s.S) - p.row0 : 0;
         all = (int)(left < 0 ? 0 : left < r.rows ? left : r.rows);
-        each = all / (unsigned)p.lanes;
+        each = p.by_lanes(all);
         extra = all - each * p.lanes;
     }
     __device__ __forceinline__ int of(int lane) const { return each + (lane < extra ? 1 : 0); }
@@ -148,15 +154,26 @@ __device__ __forceinline__ void each_group(unsigned steps, const float2* first, 
 #pragma unroll
     for (int e = 0; e < R::kEntries; ++e) set(e, first[steps >> (3 * e) & 7u]);
 }
-// Gamma and beta of a thread's column.
+// Gamma and beta of a thread's column.  What is read outside the slots is asked for before their copies, behind which it would wait for
+// thousands of cycles, and looked at after them.
 template <typename IO, typename R>
-__device__ __forceinline__ void parameters(const NormShape& s, const ResidentNorm& r, const Post& p, const IO* gammas, const IO* betas, R* gamma, R* beta) {
-    const int first = r.tuple(p.column * NormIo<IO>::kVec), block = p.first_group * (s.C / s.groups);
-    R::each(first, p.column * NormIo<IO>::kVec - first * s.T, s.T, [&](int e, int channel) {
-        gamma->set(e, p.active && gammas ? NormIo<IO>::one(gammas, block + channel) : 1.0f);
-        beta->set(e, p.active && betas ? NormIo<IO>::one(betas, block + channel) : 0.0f);
-    });
-}
+struct Parameters {
+    IO gamma[R::kEntries], beta[R::kEntries];
+    __device__ __forceinline__ void load(const NormShape& s, const ResidentNorm& r, const Post& p, const IO* gammas, const IO* betas) {
+        const int first = r.tuple(p.column * NormIo<IO>::kVec), block = p.first_group * (s.C / s.groups);
+        R::each(first, p.column * NormIo<IO>::kVec - first * s.T, s.T, [&](int e, int channel) {
+            if (p.active && gammas) gamma[e] = gammas[block + channel];
+            if (p.active && betas) beta[e] = betas[block + channel];
+        });
+    }
+    __device__ __forceinline__ void get(const Post& p, const IO* gammas, const IO* betas, R* g, R* b) const {
+#pragma unroll
+        for (int e = 0; e < R::kEntries; ++e) {
+            g->set(e, p.active && gammas ? NormIo<IO>::one(gamma, e) : 1.0f);
+            b->set(e, p.active && betas ? NormIo<IO>::one(beta, e) : 0.0f);
+        }
+    }
+};
 
 // N: see Runs.
 template <typename IO, int ACT, int N, int THREADS, int CTAS>
@@ -174,12 +191,12 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_norm_kernel(NormShape 
     uint4* slot = m.slots + threadIdx.x;
     Rows rows(s, r, p, lengths, p.b);
     int mine = p.active ? rows.of(p.lane) : 0;
+    Parameters<IO, Runs<N, P>> raw;
+    raw.load(s, r, p, gammas, betas);
     {
         const uint4* from = x + p.at(s, p.b);
         refill(0, mine, [](int) {}, [&](int i) { copy_async16(slot + i * pitch, from); from += step; });
     }
-    Runs<N, P> gamma, beta;
-    parameters(s, r, p, gammas, betas, &gamma, &beta);
     const bool whole = N == 1 || s.width % V == 0;            // a vector lies in one group
     const int group = r.width(p.column * V);                  // of the block, that of the first element
     const unsigned steps = group_steps<Runs<N, P>>(s, p.column * V - group * s.width);
@@ -272,7 +289,8 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_norm_kernel(NormShape 
             }
             __syncthreads();
         }
-        Runs<N, P> mean, scale;
+        Runs<N, P> mean, scale, gamma, beta;
+        raw.get(p, gammas, betas, &gamma, &beta);
         each_group<Runs<N, P>>(steps, m.result + group, [&](int e, float2 v) {
             mean.set(e, v.x);
             scale.set(e, v.y);
@@ -315,6 +333,15 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
     const int pitch = 2 * blockDim.x, second = blockDim.x;    // x and dy of a row are neighbours
     Rows rows(s, r, p, lengths, p.b);
     int mine = p.active ? rows.of(p.lane) : 0;
+    const int group = r.width(p.column * V);                  // of the block, that of the first element
+    const unsigned steps = group_steps<Runs<N, P>>(s, p.column * V - group * s.width);
+    const int each = s.C / s.groups, channels = p.groups * each, row = p.columns * r.sums;
+    Parameters<IO, Runs<N, P>> raw;
+    raw.load(s, r, p, gammas, betas);
+    float2 saved[Runs<N, P>::kEntries];                       // mean and rstd of the column's groups
+    each_group<Runs<N, P>>(steps, stats + p.b * s.groups + p.first_group + group, [&](int e, float2 v) { saved[e] = v; });
+    IO weight{};                                              // gamma of the first channel that this lane adds up for its warp's first group
+    if (gammas && warp < p.groups && lane < each) weight = gammas[(p.first_group + warp) * each + lane];
     {
         const uint4 *from_x = x + p.at(s, p.b), *from_dy = dy + p.at(s, p.b);
         refill(0, mine, [](int) {}, [&](int i) {
@@ -325,10 +352,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
         });
     }
     Runs<N, P> gamma, beta;
-    parameters(s, r, p, gammas, betas, &gamma, &beta);
-    const int group = r.width(p.column * V);                  // of the block, that of the first element
-    const unsigned steps = group_steps<Runs<N, P>>(s, p.column * V - group * s.width);
-    const int each = s.C / s.groups, channels = p.groups * each, row = p.columns * r.sums;
+    raw.get(p, gammas, betas, &gamma, &beta);
     float2* sums = m.side + blockDim.x * r.sums;              // a channel's, of this instance and of all so far
     float2* total = sums + r.groups * each;
     const int teams = blockDim.x / (unsigned)r.share, team = threadIdx.x / (unsigned)r.share;
@@ -337,10 +361,11 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
     for (int64_t b = p.b; b < s.B; b += r.instances, ++round) {
         // z = (x - mean) * (rstd * gamma) + beta;  rstd comes to the sums of dz * (x - mean) at the end
         Runs<N, P> mean, scale, rstd;
-        each_group<Runs<N, P>>(steps, stats + b * s.groups + p.first_group + group, [&](int e, float2 v) {
-            mean.set(e, v.x);
-            rstd.set(e, v.y);
-        });
+#pragma unroll
+        for (int e = 0; e < Runs<N, P>::kEntries; ++e) {
+            mean.set(e, saved[e].x);
+            rstd.set(e, saved[e].y);
+        }
 #pragma unroll
         for (int j = 0; j < N; ++j) scale.v[j] = mul2(rstd.v[j], gamma.v[j]);
         float2 db[P] = {}, dg[P] = {}, xc[P], dz[P];
@@ -417,7 +442,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
         for (int g = warp; g < p.groups; g += blockDim.x >> 5) {
             float2 v = make_float2(0.0f, 0.0f);
             for (int c = lane; c < each; c += 32) {
-                const float w = gammas ? NormIo<IO>::one(gammas, (p.first_group + g) * each + c) : 1.0f;
+                const float w = !gammas ? 1.0f : g == warp && c == lane ? NormIo<IO>::one(&weight, 0) : NormIo<IO>::one(gammas, (p.first_group + g) * each + c);
                 v = fma2(pair(w), sums[g * each + c], v);
             }
             v.x = warp_sum(v.x);
@@ -452,6 +477,8 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
         }
         const Rows next = lengths || b + r.instances >= s.B ? Rows(s, r, p, lengths, b + r.instances) : rows;
         const int count_next = p.active ? next.of(p.lane) : 0;
+        if (b + r.instances < s.B)
+            each_group<Runs<N, P>>(steps, stats + (b + r.instances) * s.groups + p.first_group + group, [&](int e, float2 v) { saved[e] = v; });
         uint4* to = dx + p.at(s, b);
         const uint4 *from_x = x + p.at(s, b + r.instances), *from_dy = dy + p.at(s, b + r.instances);
         auto apply = [&](int i) {
@@ -507,6 +534,9 @@ ResidentNorm resident_norm_plan(const NormShape& s, eql_dtype_t dtype, bool back
     const int per = s.width % V == 0 ? 1 : runs_of(s.T, V) < V / 2 ? runs_of(s.T, V) : V;      // entries of a vector
     r.entry = Divisor(s.width * per / V);
     r.runs = Divisor(s.T / r.run);
+    r.columns = Divisor((unsigned)columns);
+    r.lanes = Divisor((unsigned)(r.threads / columns));
+    r.by_blocks = WideDivisor(r.blocks);
     const int channels = r.groups * (s.C / s.groups), lanes = (int)(r.threads / columns);
     const int side = backward ? r.threads * r.sums + 2 * channels : r.threads * per;
     for (r.cluster = 1; r.cluster <= kMaxCluster; r.cluster *= 2) {
@@ -526,6 +556,7 @@ ResidentNorm resident_norm_plan(const NormShape& s, eql_dtype_t dtype, bool back
         if (r.cluster == kMaxCluster) break;
     }
     if (!r.supported) return r;
+    r.by_cluster = WideDivisor(r.cluster);
     r.share = 1;
     while (r.share < 32 && r.share * 2 * channels <= r.threads) r.share *= 2;
     // One CTA after the other takes a block's instances, as many side by side as are resident together, and all about the same number.
