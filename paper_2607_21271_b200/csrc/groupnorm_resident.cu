@@ -278,11 +278,20 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_norm_kernel(NormShape 
             ptx::cluster_arrive();
             ptx::cluster_wait();
             for (int g = threadIdx.x; g < p.groups; g += blockDim.x) {
-                Moments t{0.0f, 0.0f, 0.0f};
+                // relative to the first CTA's mean, which is none of theirs where it has no rows
+                const float middle = m.from(r, round, 0, g)[1];
+                float n = 0.0f, sum = 0.0f, m2 = 0.0f;
                 for (int c = 0; c < r.cluster; ++c) {
                     const float* at = m.from(r, round, c, g);
-                    t = merge(t, Moments{at[0], at[1], at[2]});
+                    if (!(at[0] > 0.0f)) continue;
+                    const float d = at[1] - middle;
+                    n += at[0];
+                    sum = fmaf(at[0], d, sum);
+                    m2 += fmaf(at[0] * d, d, at[2]);
                 }
+                const float off = n > 0.0f ? __fdividef(sum, n) : 0.0f;
+                m2 -= sum * off;
+                const Moments t{n, middle + off, m2 < 0.0f ? 0.0f : m2};
                 const float2 out = make_float2(t.mean, rstd_of(t, s.eps));
                 m.result[g] = out;
                 if (stats && p.rank == 0) stats[b * s.groups + p.first_group + g] = out;
@@ -340,8 +349,6 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
     raw.load(s, r, p, gammas, betas);
     float2 saved[Runs<N, P>::kEntries];                       // mean and rstd of the column's groups
     each_group<Runs<N, P>>(steps, stats + p.b * s.groups + p.first_group + group, [&](int e, float2 v) { saved[e] = v; });
-    IO weight{};                                              // gamma of the first channel that this lane adds up for its warp's first group
-    if (gammas && warp < p.groups && lane < each) weight = gammas[(p.first_group + warp) * each + lane];
     {
         const uint4 *from_x = x + p.at(s, p.b), *from_dy = dy + p.at(s, p.b);
         refill(0, mine, [](int) {}, [&](int i) {
@@ -353,8 +360,8 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
     }
     Runs<N, P> gamma, beta;
     raw.get(p, gammas, betas, &gamma, &beta);
-    float2* sums = m.side + blockDim.x * r.sums;              // a channel's, of this instance and of all so far
-    float2* total = sums + r.groups * each;
+    const bool whole = N == 1 || s.width % V == 0;            // a vector lies in one group
+    float2* total = m.side + blockDim.x * (r.sums + (whole ? 1 : Runs<N, P>::kEntries));      // a channel's sums over all instances so far
     const int teams = blockDim.x / (unsigned)r.share, team = threadIdx.x / (unsigned)r.share;
     for (int c = threadIdx.x; c < channels; c += blockDim.x) total[c] = make_float2(0.0f, 0.0f);
     int round = 0;
@@ -398,61 +405,82 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
 #pragma unroll 2
         for (int i = half; i < mine; ++i) add(i);
 
-        // The thread's sums side by side: r.sums of them, of r.run neighbouring elements each (a channel's).
+        // The thread's sums side by side: r.sums of them, of r.run neighbouring elements each (a channel's); and times gamma, for the
+        // groups, of its vector or where groups cross that of its runs.
+        float2* weighted = m.side + blockDim.x * r.sums;
         if (N == 1) {
             db[0] = add2(db[0], db[1]);
             dg[0] = mul2(add2(dg[0], dg[1]), rstd.v[0]);
-            m.side[threadIdx.x] = make_float2(db[0].x + db[0].y, dg[0].x + dg[0].y);
+            const float2 v = make_float2(db[0].x + db[0].y, dg[0].x + dg[0].y);
+            m.side[threadIdx.x] = v;
+            weighted[threadIdx.x] = mul2(v, gamma.v[0]);
         } else {
+            float2 all1 = pair(0.0f), all2 = pair(0.0f);
+            float2 *to = m.side + threadIdx.x * r.sums, *each_weighted = weighted + threadIdx.x * Runs<N, P>::kEntries;
 #pragma unroll
             for (int j = 0; j < N; ++j) {
                 dg[j] = mul2(dg[j], rstd.v[j]);
-                float2* to = m.side + threadIdx.x * r.sums;
+                const float2 w1 = mul2(db[j], gamma.v[j]), w2 = mul2(dg[j], gamma.v[j]);
                 if (r.sums <= N) {
                     to[j] = make_float2(db[j].x + db[j].y, dg[j].x + dg[j].y);
                 } else {                                      // (each half of a pair is a channel's)
                     to[2 * j] = make_float2(db[j].x, dg[j].x);
                     to[2 * j + 1] = make_float2(db[j].y, dg[j].y);
                 }
-            }
-        }
-        __syncthreads();
-        // Channels: `share` lanes each, over the lanes of rows and the runs of the tuple.
-        const int entries = min(p.lanes, rows.all) * (int)r.runs.d;
-        for (int c0 = 0; c0 < channels; c0 += teams) {
-            const int c = c0 + team;
-            float2 v = make_float2(0.0f, 0.0f);
-            if (c < channels)
-                for (int e = threadIdx.x - team * r.share; e < entries; e += r.share) {
-                    const int l = r.runs(e);
-                    v = add2(v, m.side[l * row + (c - l) * (int)r.runs.d + e]);
+                if (whole) {
+                    all1 = add2(all1, w1);
+                    all2 = add2(all2, w2);
+                } else if (N < P) {
+                    each_weighted[j] = make_float2(w1.x + w1.y, w2.x + w2.y);
+                } else {
+                    each_weighted[2 * j] = make_float2(w1.x, w2.x);
+                    each_weighted[2 * j + 1] = make_float2(w1.y, w2.y);
                 }
-            for (int d = r.share >> 1; d > 0; d >>= 1) {
-                v.x += __shfl_xor_sync(0xffffffffu, v.x, d);
-                v.y += __shfl_xor_sync(0xffffffffu, v.y, d);
             }
-            if (c < channels && threadIdx.x == team * r.share) {
-                sums[c] = v;
-                total[c] = add2(total[c], v);
-            }
+            if (whole) weighted[threadIdx.x] = make_float2(all1.x + all1.y, all2.x + all2.y);
         }
         __syncthreads();
         if (r.cluster > 1 && round == 0) ptx::cluster_wait();
         const float count = (float)positions_of(lengths, b, s.S) * s.width, share = count > 0.0f ? __fdividef(1.0f, count) : 0.0f;
+        const int row_lanes = min(p.lanes, rows.all), per = whole ? 1 : Runs<N, P>::kEntries;
+        // Channels: `share` lanes each, over the lanes of rows and the runs of the tuple.
+        auto add_channels = [&]() {
+            const int entries = row_lanes * (int)r.runs.d;
+            for (int c0 = 0; c0 < channels; c0 += teams) {
+                const int c = c0 + team;
+                float2 v = make_float2(0.0f, 0.0f);
+                if (c < channels)
+                    for (int e = threadIdx.x - team * r.share; e < entries; e += r.share) {
+                        const int l = r.runs(e);
+                        v = add2(v, m.side[l * row + (c - l) * (int)r.runs.d + e]);
+                    }
+#pragma unroll
+                for (int d = 16; d > 0; d >>= 1)
+                    if (d < r.share) {
+                        v.x += __shfl_xor_sync(0xffffffffu, v.x, d);
+                        v.y += __shfl_xor_sync(0xffffffffu, v.y, d);
+                    }
+                if (c < channels && threadIdx.x == team * r.share) total[c] = add2(total[c], v);
+            }
+        };
         for (int g = warp; g < p.groups; g += blockDim.x >> 5) {
+            const int width = (int)r.entry.d;                 // entries of the group in a lane of rows
             float2 v = make_float2(0.0f, 0.0f);
-            for (int c = lane; c < each; c += 32) {
-                const float w = !gammas ? 1.0f : g == warp && c == lane ? NormIo<IO>::one(&weight, 0) : NormIo<IO>::one(gammas, (p.first_group + g) * each + c);
-                v = fma2(pair(w), sums[g * each + c], v);
+            for (int e = lane; e < row_lanes * width; e += 32) {
+                const int l = r.entry(e);
+                v = add2(v, weighted[l * p.columns * per + (g - l) * width + e]);
             }
             v.x = warp_sum(v.x);
             v.y = warp_sum(v.y);
             if (r.cluster > 1) m.send(r, round, p.rank, g, v.x, v.y, 0.0f);
             else if (lane == 0) m.result[g] = make_float2(v.x * share, v.y * share);
         }
+        if (r.cluster == 1) add_channels();
         __syncthreads();
+        if (r.cluster > 1) ptx::cluster_arrive();
+        if (r.cluster > 1) add_channels();                    // while the other CTAs come
         if (r.cluster > 1) {
-            ptx::cluster_arrive();
+            __syncwarp();
             ptx::cluster_wait();
             for (int g = threadIdx.x; g < p.groups; g += blockDim.x) {
                 float2 v = make_float2(0.0f, 0.0f);
@@ -538,7 +566,7 @@ ResidentNorm resident_norm_plan(const NormShape& s, eql_dtype_t dtype, bool back
     r.lanes = Divisor((unsigned)(r.threads / columns));
     r.by_blocks = WideDivisor(r.blocks);
     const int channels = r.groups * (s.C / s.groups), lanes = (int)(r.threads / columns);
-    const int side = backward ? r.threads * r.sums + 2 * channels : r.threads * per;
+    const int side = backward ? r.threads * (r.sums + per) + channels : r.threads * per;
     for (r.cluster = 1; r.cluster <= kMaxCluster; r.cluster *= 2) {
         r.rows = (s.S + r.cluster - 1) / r.cluster;
         const int64_t slots = (r.rows + lanes - 1) / lanes, slot_bytes = slots * r.threads * 16 * (backward ? 2 : 1);
