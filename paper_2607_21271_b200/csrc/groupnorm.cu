@@ -178,7 +178,7 @@ struct Column {
 #pragma unroll
         for (int j = 0; j < P; ++j) {
             xc[j] = sub2(xc[j], mean.of(j));
-            if (ACT != EQL_ACT_NONE) dz[j] = mul2(dz[j], slope<ACT>(fma2(xc[j], scale.of(j), beta.of(j))));
+            if (ACT != EQL_ACT_NONE) dz[j] = mul2(dz[j], slope<ACT, (N < P)>(fma2(xc[j], scale.of(j), beta.of(j))));
         }
     }
 };
@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(kThreads, range_ctas(N, NormIo<IO>::kVec / 2))
                 float2 f[V / 2];
                 NormIo<IO>::widen(u[0], f);
 #pragma unroll
-                for (int j = 0; j < V / 2; ++j) f[j] = activate<ACT>(fma2(sub2(f[j], c.mean.of(j)), c.scale.of(j), c.beta.of(j)));
+                for (int j = 0; j < V / 2; ++j) f[j] = activate<ACT, (N < V / 2)>(fma2(sub2(f[j], c.mean.of(j)), c.scale.of(j), c.beta.of(j)));
                 y[at + i * step] = NormIo<IO>::narrow(f);
             });
 }

@@ -315,7 +315,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_norm_kernel(NormShape 
             float2 f[P];
             NormIo<IO>::widen(slot[i * pitch], f);
 #pragma unroll
-            for (int j = 0; j < P; ++j) f[j] = activate<ACT>(fma2(sub2(f[j], mean.of(j)), scale.of(j), beta.of(j)));
+            for (int j = 0; j < P; ++j) f[j] = activate<ACT, (N < P)>(fma2(sub2(f[j], mean.of(j)), scale.of(j), beta.of(j)));
             *to = NormIo<IO>::narrow(f);
             to += step;
         };
@@ -384,7 +384,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_gradient_kernel(NormSh
 #pragma unroll
             for (int j = 0; j < P; ++j) {
                 xc[j] = sub2(xc[j], mean.of(j));
-                if (ACT != EQL_ACT_NONE && !(kKeep && again)) dz[j] = mul2(dz[j], slope<ACT>(fma2(xc[j], scale.of(j), beta.of(j))));
+                if (ACT != EQL_ACT_NONE && !(kKeep && again)) dz[j] = mul2(dz[j], slope<ACT, (N < P)>(fma2(xc[j], scale.of(j), beta.of(j))));
             }
         };
         auto add = [&](int i) {

@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(threads_for(NV), forward_ctas(NV, TUPLE)) warp
                 gamma[k].widen(ga);
                 beta[k].widen(be);
 #pragma unroll
-                for (int j = 0; j < P; ++j) f[k][j] = activate<ACT>(fma2(f[k][j], mul2(ga[j], pair(rstd)), be[j]));
+                for (int j = 0; j < P; ++j) f[k][j] = activate<ACT, TUPLE>(fma2(f[k][j], mul2(ga[j], pair(rstd)), be[j]));
                 y[b * s.S * s.vectors + v.at[k]] = NormIo<IO>::narrow(f[k]);
             }
     }
@@ -195,7 +195,7 @@ __global__ void __launch_bounds__(threads_for(NV), gradient_ctas(NV, SUMS)) warp
 #pragma unroll
                 for (int j = 0; j < P; ++j) {
                     const float2 xh = mul2(sub2(xc[k][j], pair(mean)), pair(rstd));
-                    if (ACT != EQL_ACT_NONE) dz[k][j] = mul2(dz[k][j], slope<ACT>(fma2(xh, ga[j], be[j])));
+                    if (ACT != EQL_ACT_NONE) dz[k][j] = mul2(dz[k][j], slope<ACT, (SUMS < P)>(fma2(xh, ga[j], be[j])));
                     float2 &b_sum = db[k][j * SUMS / P], &g_sum = dg[k][j * SUMS / P];
                     b_sum = add2(b_sum, dz[k][j]);
                     g_sum = fma2(dz[k][j], xh, g_sum);

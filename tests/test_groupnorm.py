@@ -354,23 +354,35 @@ def test_values_far_from_zero_and_single_far_values(shape):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("act", ["gelu", "silu"])
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
-@pytest.mark.parametrize("shape", [(8, 96, 32, 3, 197), (16, 64, 1, 20, 1), (4, 24, 2, 2, 3000), (1, 320, 32, 2, 49)])
-def test_what_is_not_finite_stays_in_its_group(shape, bad):
+@pytest.mark.parametrize("shape", [(8, 96, 32, 3, 197), (16, 64, 1, 20, 1), (4, 24, 2, 2, 3000), (1, 320, 32, 2, 49), (3, 16, 16, 2, 60), (4, 24, 8, 1, 20000)])
+def test_what_is_not_finite_stays_in_its_group(shape, bad, act):
     T, C, groups, B, S = shape
-    n = Norm(*shape, "fp16", "gelu", seed=7)
+    n = Norm(*shape, "fp16", act, seed=7)
     n.fwd()
     n.bwd()
     good = n.outputs()
-    n.x[1, S // 2, 3] = bad
+    n.x[B - 1, S // 2, 2] = bad
     n.fwd()
     n.bwd()
     now = n.outputs()
     w = C * T // groups
     hit = torch.zeros_like(now["y"], dtype=torch.bool)
-    hit[1, :, :w] = True
+    hit[B - 1, :, :w] = True
     for k in ("y", "dx"):
         assert bool(torch.isnan(now[k][hit]).all()) and torch.equal(now[k][~hit], good[k][~hit])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("shape", [(8, 96, 32, 2, 197), (16, 64, 1, 20, 1), (4, 24, 1, 1, 5000), (1, 320, 32, 2, 49), (4, 32, 4, 9, 2)])
+def test_activations_far_from_zero(shape, dtype, act):
+    """Arguments of hundreds on either side, where exponentials leave float and a pair of values holds both ends."""
+    n = Norm(*shape, dtype, act, seed=12)
+    n.gamma.mul_(150.0)
+    n.step()
 
 
 @pytest.mark.gpu
