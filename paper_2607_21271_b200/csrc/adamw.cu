@@ -690,7 +690,7 @@ eql_status_t eqlinear_adamw_clip(eqlinear_adamw_t opt, float max_norm, const flo
 
 eql_status_t eqlinear_adamw_step(eqlinear_adamw_t opt, double lr, double beta1, double beta2, double eps, const float* lr_device, void* stream) {
     if (eql_status_t st = check_optimiser(opt); st != EQL_OK) return st;
-    if (!(lr >= 0.0) || !std::isfinite(lr) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0)) return EQL_ERR_INVALID_ARG;
+    if (!(lr >= 0.0) || !std::isfinite((float)lr) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0)) return EQL_ERR_INVALID_ARG;
     if (!((float)eps >= FLT_MIN) || !std::isfinite((float)eps)) return EQL_ERR_INVALID_ARG;
     if (!aligned(lr_device, 4)) return EQL_ERR_ALIGNMENT;
     const Rates r{(float)lr, (float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps, 1.0f, std::log(beta1), std::log(beta2), lr_device};

@@ -34,7 +34,7 @@ struct WarpNorm {
     int group_blocks, ctas;   // CTAs that cover all groups, and how many such sets there are
     int sums, shared_bytes;
 };
-constexpr int kWarpNormShared = 66 * 1024;        // 256 lanes x 4 vectors x 8 sums x 8 bytes, and some
+constexpr int kWarpNormShared = 32 * 1024;        // 256 lanes x 2 vectors (128 x 4) x 8 sums x 8 bytes
 WarpNorm warp_norm_plan(const NormShape& s, eql_dtype_t dtype, bool backward);
 cudaError_t launch_warp_norm(const NormShape& s, const WarpNorm& w, eql_dtype_t dtype, const void* x, const void* gamma, const void* beta,
                              const int32_t* lengths, void* y, float* stats, cudaStream_t stream);

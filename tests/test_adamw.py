@@ -348,7 +348,7 @@ def test_first_step_from_empty_states_and_edges_of_the_rates():
         torch.cuda.synchronize()
         assert all(torch.equal(a, t["p"]) for a, t in zip(kept, o.parts))
         for bad in (dict(lr=-1e-3), dict(lr=math.nan), dict(lr=1e-3, beta1=1.0), dict(lr=1e-3, beta2=-0.1), dict(lr=1e-3, eps=0.0),
-                    dict(lr=1e-3, eps=1e-60), dict(lr=1e-3, eps=math.inf), dict(lr=math.inf)):
+                    dict(lr=1e-3, eps=1e-60), dict(lr=1e-3, eps=1e-40), dict(lr=1e-3, eps=math.inf), dict(lr=math.inf), dict(lr=1e39)):
             with pytest.raises(eq.EqlError) as e:
                 eq.eqlinear_adamw_step(o.h, **bad)
             assert e.value.status == binding.EQL_ERR_INVALID_ARG
