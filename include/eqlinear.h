@@ -405,8 +405,9 @@ eql_status_t eqlinear_adamw_workspace_bytes(const eql_adamw_tensor_t* tensors, i
 /* Build an optimiser on the current device over `count` tensors (host array, copied).  Its table of tensors and its step
  * counter (0) live in `workspace` (device, 256-byte aligned, the caller's, untouched until eqlinear_adamw_destroy).  No two
  * of the buffers that a step writes may share bytes, nor may one share bytes with a gradient or the workspace
- * (EQL_ERR_INVALID_ARG); nor may one be memory of the host or of another device.  The table travels over `stream`, which is synchronised: not during stream capture
- * (EQL_ERR_INVALID_ARG).  On error *opt is set to NULL. */
+ * (EQL_ERR_INVALID_ARG); nor may one, or the workspace, be memory of the host or of another device (EQL_ERR_INVALID_ARG).  The
+ * table travels over `stream`, which is synchronised: not during stream capture (EQL_ERR_INVALID_ARG).  On error *opt is
+ * set to NULL. */
 eql_status_t eqlinear_adamw(eqlinear_adamw_t* opt, const eql_adamw_tensor_t* tensors, int count, int state_bits,
                             void* workspace, size_t workspace_bytes, void* stream);
 
@@ -429,7 +430,7 @@ eql_status_t eqlinear_adamw_step(eqlinear_adamw_t opt, double lr, double beta1, 
 /* Sets the number of steps taken (asynchronous on `stream`), e.g. after loading a checkpoint; forgets a pending clip. */
 eql_status_t eqlinear_adamw_set_step(eqlinear_adamw_t opt, int64_t step, void* stream);
 
-/* Reads the counters back (synchronises `stream`). */
+/* Reads the counters back (synchronises `stream`: EQL_ERR_INVALID_ARG during its capture). */
 eql_status_t eqlinear_adamw_info(eqlinear_adamw_t opt, eql_adamw_info_t* info, void* stream);
 
 /* Frees the host object only (the workspace is the caller's).  NULL is accepted. */

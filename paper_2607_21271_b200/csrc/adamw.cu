@@ -548,16 +548,24 @@ eql_status_t check_tensor(const eql_adamw_tensor_t& t, int state_bits, Range* ra
     return EQL_OK;
 }
 
-// Whether all of a tensor's buffers are memory of `device`: a kernel that met another pointer would fault.
+// Whether a pointer is memory of `device` (or none): a kernel that met another one would fault.
+bool on_device(const void* p, int device) {
+    if (!p) return true;
+    cudaPointerAttributes a{};
+    if (cudaPointerGetAttributes(&a, p) != cudaSuccess) { cudaGetLastError(); return false; }
+    return a.type == cudaMemoryTypeManaged || (a.type == cudaMemoryTypeDevice && a.device == device);
+}
 bool on_device(const eql_adamw_tensor_t& t, int device) {
-    const void* pointers[] = {t.param, t.master, t.grad, t.exp_avg, t.exp_avg_sq, t.exp_avg_scale, t.exp_avg_sq_scale};
-    for (const void* p : pointers) {
-        if (!p) continue;
-        cudaPointerAttributes a{};
-        if (cudaPointerGetAttributes(&a, p) != cudaSuccess) { cudaGetLastError(); return false; }
-        if (a.type != cudaMemoryTypeManaged && (a.type != cudaMemoryTypeDevice || a.device != device)) return false;
-    }
+    for (const void* p : {(const void*)t.param, (const void*)t.master, (const void*)t.grad, (const void*)t.exp_avg, (const void*)t.exp_avg_sq,
+                          (const void*)t.exp_avg_scale, (const void*)t.exp_avg_sq_scale})
+        if (!on_device(p, device)) return false;
     return true;
+}
+// Calls that wait for a stream cannot be captured.
+eql_status_t not_capturing(cudaStream_t s) {
+    cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(s, &capturing) != cudaSuccess) return EQL_ERR_CUDA;
+    return capturing == cudaStreamCaptureStatusNone ? EQL_OK : EQL_ERR_INVALID_ARG;
 }
 
 // Whether a written range shares bytes with any other.
@@ -642,12 +650,11 @@ eql_status_t eqlinear_adamw(eqlinear_adamw_t* opt, const eql_adamw_tensor_t* ten
     if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) return EQL_ERR_CUDA;
     if (major != 10) return EQL_ERR_ARCH;
     if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return EQL_ERR_CUDA;
+    if (!on_device(workspace, dev)) return EQL_ERR_INVALID_ARG;
     for (int i = 0; i < count; ++i)
         if (tensors[i].numel > 0 && !on_device(tensors[i], dev)) return EQL_ERR_INVALID_ARG;
     const cudaStream_t s = (cudaStream_t)stream;
-    cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
-    if (cudaStreamIsCapturing(s, &capturing) != cudaSuccess) return EQL_ERR_CUDA;
-    if (capturing != cudaStreamCaptureStatusNone) return EQL_ERR_INVALID_ARG;
+    if (eql_status_t c = not_capturing(s); c != EQL_OK) return c;
 
     char* image = static_cast<char*>(std::calloc(1, lay.total));
     if (!image) return EQL_ERR_INVALID_ARG;
@@ -711,6 +718,7 @@ eql_status_t eqlinear_adamw_set_step(eqlinear_adamw_t opt, int64_t step, void* s
 eql_status_t eqlinear_adamw_info(eqlinear_adamw_t opt, eql_adamw_info_t* info, void* stream) {
     if (eql_status_t st = check_optimiser(opt); st != EQL_OK) return st;
     if (!info) return EQL_ERR_INVALID_ARG;
+    if (eql_status_t st = not_capturing((cudaStream_t)stream); st != EQL_OK) return st;
     Control c{};
     if (cudaMemcpyAsync(&c, opt->ws, sizeof(c), cudaMemcpyDeviceToHost, (cudaStream_t)stream) != cudaSuccess) return EQL_ERR_CUDA;
     if (cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess) return EQL_ERR_CUDA;

@@ -464,3 +464,35 @@ def test_memory_of_the_host_is_refused(which):
         workspace = torch.empty(bytes_, dtype=torch.uint8, device="cuda")
         assert refused(table, 8, workspace, bytes_) == binding.EQL_ERR_INVALID_ARG
     torch.cuda.synchronize()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("pinned", [False, True])
+def test_a_workspace_of_the_host_is_refused(pinned):
+    args = {k: torch.zeros(512, device="cuda") for k in ("param", "grad", "exp_avg", "exp_avg_sq")}
+    table = [eq.eqlinear_adamw_tensor(**args, numel=512, param_dtype=eq.EQL_FP32, grad_dtype=eq.EQL_FP32)]
+    bytes_ = eq.eqlinear_adamw_workspace_bytes(table, 32)
+    host = torch.zeros(bytes_ + 256, dtype=torch.uint8)
+    host = host.pin_memory() if pinned else host
+    assert refused(table, 32, host[-host.data_ptr() % 256:], bytes_) == binding.EQL_ERR_INVALID_ARG
+    assert not host.any()
+
+
+@pytest.mark.gpu
+def test_counters_are_not_read_during_capture():
+    """The call waits for its stream: refused, and the capture goes on."""
+    o = Optimiser((300,), "fp32", "fp32", 32, False, seed=12)
+    try:
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            s = torch.cuda.current_stream().cuda_stream
+            eq.eqlinear_adamw_step(o.h, 1e-3, stream=s)
+            with pytest.raises(eq.EqlError) as e:
+                eq.eqlinear_adamw_info(o.h, s)
+            assert e.value.status == binding.EQL_ERR_INVALID_ARG
+        graph.replay()
+        torch.cuda.synchronize()
+        assert eq.eqlinear_adamw_info(o.h, o.stream).step == 1
+    finally:
+        o.close()
