@@ -217,13 +217,14 @@ __device__ __forceinline__ int64_t positions_of(const int32_t* lengths, int64_t 
 __device__ __forceinline__ float2 minus_abs(float2 v) { return make_float2(-fabsf(v.x), -fabsf(v.y)); }
 
 // 1 / (1 + exp(-z)), good to 2^-22.  TOGETHER: by one reciprocal of the pair's product, which the two values then turn into each other's, so
-// that the special-function unit has a quarter less to do; exp(-z) is held to 2^60 for it, and a NaN of one reaches the other, so it is
-// for pairs of one channel.  (128 x 197 x 768 bfloat16 with SiLU, forward and backward: 59.3 -> 57.9 us.  GELU, whose polynomial keeps
-// the multiplying units as busy, does not gain: 128 x 3136 x 384 490 -> 494.)
-template <bool TOGETHER> __device__ __forceinline__ float2 sigmoid(float2 z) {
-    const float2 e = mul2(z, pair(-1.44269504088896341f));
-    if (!TOGETHER) return reciprocal(add2(exp2_fast(e), pair(1.0f)));
-    const float2 d = add2(exp2_fast(make_float2(fminf(e.x, 60.0f), fminf(e.y, 60.0f))), pair(1.0f));
+// that the special-function unit has a quarter less to do; z is held at -41.5 from below for it, so that the product stays a float's (for
+// the caller too: what the sigmoid is multiplied by must not grow on), and a NaN of one reaches the other, so it is for pairs of one
+// channel.  (128 x 197 x 768 bfloat16 with SiLU, forward and backward: 59.3 -> 58.1 us.  GELU, whose polynomial keeps the multiplying
+// units as busy, does not gain: 128 x 3136 x 384 490 -> 494.)
+template <bool TOGETHER> __device__ __forceinline__ float2 sigmoid(float2& z) {
+    if (TOGETHER) z = make_float2(fmax_nan(z.x, -41.5f), fmax_nan(z.y, -41.5f));
+    const float2 d = add2(exp2_fast(mul2(z, pair(-1.44269504088896341f))), pair(1.0f));
+    if (!TOGETHER) return reciprocal(d);
     return mul2(pair(reciprocal(d.x * d.y)), make_float2(d.y, d.x));
 }
 // Phi(-|z|) = erfc(|z| / sqrt 2) / 2 by the rational approximation 7.1.26 of Abramowitz and Stegun (error of erfc at most 1.5e-7, a float's
@@ -247,7 +248,10 @@ template <int ACT, bool TOGETHER> __device__ __forceinline__ float2 activate(flo
         const float2 q = tail_of_normal(z, &density);
         return fma2(minus_abs(z), q, make_float2(fmaxf(z.x, 0.0f), fmaxf(z.y, 0.0f)));
     }
-    if (ACT == EQL_ACT_SILU) return mul2(z, sigmoid<TOGETHER>(z));
+    if (ACT == EQL_ACT_SILU) {
+        const float2 p = sigmoid<TOGETHER>(z);
+        return mul2(z, p);
+    }
     return z;
 }
 template <int ACT, bool TOGETHER> __device__ __forceinline__ float2 slope(float2 z) {

@@ -440,3 +440,31 @@ def test_the_same_bits_again_on_another_stream_and_replayed(shape):
             assert all(torch.equal(got[k], want[k]) for k in want)
     a.guard.check()
     b.guard.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("shape", [(8, 96, 32, 2, 197), (16, 64, 1, 20, 1), (4, 24, 8, 1, 20000), (1, 320, 32, 2, 49), (4, 32, 4, 9, 2)])
+def test_arguments_beyond_any_exponential(shape, dtype, act):
+    """Arguments of 1e25: the activations are 0 and z there, their slopes 0 and 1."""
+    n = Norm(*shape, dtype, act, seed=13)
+    n.gamma.fill_(1e25)
+    n.fwd()
+    n.bwd()
+    n.guard.check()
+    T, C, groups, B, S = shape
+    x, dy = (t.double().view(B, S, groups, -1) for t in (n.x, n.dy))
+    mean, rstd = (n.stats[..., k].double().view(B, 1, groups, 1) for k in (0, 1))
+    z = float(n.gamma[0]) * (x - mean) * rstd
+    y, up = n.y.double().view_as(z), z > 0
+    assert float(z.abs().min()) > 1e6                                                 # (beta, 0.3, and the mean's rounding do not count)
+    # below: |z| sigmoid(z) and its like fall from 1e-16 on past any z that the kernels may hold them at
+    assert float(y[~up].abs().max()) < 1e-15
+    # above: two roundings of float on either side of a subtraction, of values up to max |x|, and the output's own
+    near = z.abs() + float(n.gamma[0]) * rstd * x.abs().amax()
+    half = torch.finfo(n.y.dtype).eps / 2
+    assert bool(((y - z)[up].abs() <= (2.0 ** -20 * near + half * z.abs() + 1)[up]).all())
+    want = torch.where(up, dy, 0).view(B, S, C, T)
+    size = want.abs().sum((0, 1, 3))
+    assert bool(((n.dbeta.double() - want.sum((0, 1, 3))).abs() <= (B * S * T * 2.0 ** -24 + 2.0 ** -20) * size + 1e-12).all())
