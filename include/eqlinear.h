@@ -412,7 +412,7 @@ eql_status_t eqlinear_adamw(eqlinear_adamw_t* opt, const eql_adamw_tensor_t* ten
                             void* workspace, size_t workspace_bytes, void* stream);
 
 /* The global gradient norm, for the next eqlinear_adamw_step: with n = sqrt(sum of all g^2) / *loss_scale, that step uses
- * f = min(1, max_norm / (n + 1e-6)) / *loss_scale, and is left out (no parameter, state or step number changes) where n or the
+ * f = min(1, max_norm / (n + 1e-6)) / *loss_scale, and is left out (no parameter, state or step number changes) where n, f or the
  * loss scale is not finite or the loss scale is not above zero.
  *   max_norm    > 0; infinity bounds nothing
  *   loss_scale  device float, read when the kernel runs, or NULL for 1

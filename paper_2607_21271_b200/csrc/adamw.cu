@@ -482,10 +482,11 @@ __global__ void __launch_bounds__(kAdamThreads, kNormCtasPerSm) grad_norm_kernel
     if (threadIdx.x == 0) {
         const float scale = loss_scale ? *loss_scale : 1.0f;
         const float norm = (float)(sqrt(sum) / (double)scale);
-        const bool fine = isfinite(norm) && isfinite(scale) && scale > 0.0f;
+        const float factor = __fdiv_rn(fminf(1.0f, __fdiv_rn(max_norm, __fadd_rn(norm, 1e-6f))), scale);
+        const bool fine = isfinite(norm) && isfinite(scale) && scale > 0.0f && isfinite(factor);
         control->norm = norm;
         control->skip = fine ? 0 : 1;
-        control->factor = fine ? __fdiv_rn(fminf(1.0f, __fdiv_rn(max_norm, __fadd_rn(norm, 1e-6f))), scale) : 0.0f;
+        control->factor = fine ? factor : 0.0f;
         control->norm_ticket = 0;
         if (norm_out) *norm_out = norm;
     }

@@ -496,3 +496,21 @@ def test_counters_are_not_read_during_capture():
         assert eq.eqlinear_adamw_info(o.h, o.stream).step == 1
     finally:
         o.close()
+
+
+@pytest.mark.gpu
+def test_a_loss_scale_whose_reciprocal_is_not_finite_changes_nothing():
+    """1 / 1e-40 is beyond float, and gradients of zero (norm 0) times that would be NaN."""
+    o = Optimiser((300, 7), "fp32", "fp32", 32, False, seed=13)
+    try:
+        for t in o.parts:
+            t["g"].zero_()
+        before = o.snapshot()
+        eq.eqlinear_adamw_clip(o.h, 1.0, torch.full((1,), 1e-40, device="cuda"), stream=o.stream)
+        assert eq.eqlinear_adamw_info(o.h, o.stream).skip == 1
+        eq.eqlinear_adamw_step(o.h, 1e-3, stream=o.stream)
+        info = eq.eqlinear_adamw_info(o.h, o.stream)
+        assert (info.step, info.skipped) == (0, 1)
+        assert all(torch.equal(a[k], b[k]) for a, b in zip(before, o.snapshot()) for k in a)
+    finally:
+        o.close()
