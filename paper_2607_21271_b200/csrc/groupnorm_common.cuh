@@ -64,6 +64,7 @@ struct ResidentNorm {
     int cluster, threads;     // CTAs of a unit, threads of a CTA
     int instances;            // instances that are worked on side by side
     int64_t rows;             // rows of a CTA
+    int form;                 // N of the kernels that are launched (see Runs), by which everything a thread puts side by side is laid out
     int run, sums, share;     // backward: neighbouring elements summed up in a thread, sums of a vector, lanes that add up a channel
     int slot_bytes, side_offset, shared_bytes;
     Divisor tuple, width, entry, runs;        // T; elements of a group; entries of a group in a row (its vectors, or elements); runs of a tuple
@@ -180,6 +181,8 @@ struct RunningMoments {
 };
 __device__ __forceinline__ float rstd_of(const Moments& v, float eps) { return rsqrtf((v.n > 0.0f ? __fdividef(v.m2, v.n) : 0.0f) + eps); }
 
+// Entries of a vector of P pairs in N runs: one a run, or each element for itself.
+constexpr int entries_of(int N, int P) { return N < P ? N : 2 * P; }
 // What belongs to the elements of a vector in N equal runs: channels and groups begin where runs do.  N = 1 where the vector is of one
 // channel, 2 where it is of two of half its length each, all pairs otherwise (and then each element for itself).
 template <int N, int P>
@@ -191,7 +194,7 @@ struct Runs {
         if (N < P) v[entry] = pair(value);
         else (&v[entry / 2].x)[entry % 2] = value;
     }
-    static constexpr int kEntries = N < P ? N : 2 * P, kLength = 2 * P / kEntries;      // (an entry's elements)
+    static constexpr int kEntries = entries_of(N, P), kLength = 2 * P / kEntries;      // (an entry's elements)
     // set(entry, its channel), and the same for groups, for the vector whose first element is element `at` of the channel or group `first`
     template <typename Set>
     static __device__ __forceinline__ void each(int first, int at, int length, Set&& set) {

@@ -554,12 +554,13 @@ ResidentNorm resident_norm_plan(const NormShape& s, eql_dtype_t dtype, bool back
     const int64_t columns = bytes(r.groups) / 16;
     if (columns > (backward ? kManyBackward : kManyForward)) return r;
     r.threads = columns <= kFewThreads ? kFewThreads : backward ? kManyBackward : kManyForward;
+    r.form = r.threads == kFewThreads ? runs_of(s.T, V) : V / 2;              // (with many threads there is the general form only)
     r.blocks = (s.groups + r.groups - 1) / r.groups;
     r.run = run_length(s.T, V);
     r.sums = V / r.run;
     r.tuple = Divisor(s.T);
     r.width = Divisor(s.width);
-    const int per = s.width % V == 0 ? 1 : runs_of(s.T, V) < V / 2 ? runs_of(s.T, V) : V;      // entries of a vector
+    const int per = s.width % V == 0 ? 1 : entries_of(r.form, V / 2);         // entries of a vector
     r.entry = Divisor(s.width * per / V);
     r.runs = Divisor(s.T / r.run);
     r.columns = Divisor((unsigned)columns);
@@ -589,7 +590,7 @@ ResidentNorm resident_norm_plan(const NormShape& s, eql_dtype_t dtype, bool back
     while (r.share < 32 && r.share * 2 * channels <= r.threads) r.share *= 2;
     // One CTA after the other takes a block's instances, as many side by side as are resident together, and all about the same number.
     // (A cluster takes one: how many of them are resident depends on the SMs that the device has in each of its parts.)
-    int64_t together = 228 * 1024 / (r.shared_bytes + 1024), most = backward ? kGradientCtas : forward_ctas(runs_of(s.T, V), V / 2);
+    int64_t together = 228 * 1024 / (r.shared_bytes + 1024), most = backward ? kGradientCtas : forward_ctas(r.form, V / 2);
     if (r.threads != kFewThreads) most = 1;
     if (together > most) together = most;
     together = together * kNumSMs / (r.blocks * r.cluster);
@@ -630,8 +631,8 @@ cudaError_t launch_resident_norm(const NormShape& s, const ResidentNorm& r, eql_
                 return launch_resident(kernel, limit, s, r, stream, (const uint4*)x, (const IO*)gamma, (const IO*)beta, lengths, (uint4*)y, (float2*)stats);
             };
             if (r.threads != kFewThreads) return launch(resident_norm_kernel<IO, ACT, P, kManyForward, 1>, limits[0]);
-            if (runs_of(s.T, V) == 1) return launch(resident_norm_kernel<IO, ACT, 1, kFewThreads, forward_ctas(1, P)>, limits[1]);
-            if (runs_of(s.T, V) < P) return launch(resident_norm_kernel<IO, ACT, 2, kFewThreads, forward_ctas(2, P)>, limits[2]);
+            if (r.form == 1) return launch(resident_norm_kernel<IO, ACT, 1, kFewThreads, forward_ctas(1, P)>, limits[1]);
+            if (r.form < P) return launch(resident_norm_kernel<IO, ACT, 2, kFewThreads, forward_ctas(2, P)>, limits[2]);
             return launch(resident_norm_kernel<IO, ACT, P, kFewThreads, forward_ctas(P, P)>, limits[3]);
         });
     });
@@ -650,8 +651,8 @@ cudaError_t launch_resident_gradient(const NormShape& s, const ResidentNorm& r, 
                                        (const float2*)stats, (uint4*)dx, (float2*)parts);
             };
             if (r.threads != kFewThreads) return launch(resident_gradient_kernel<IO, ACT, P, kManyBackward, 1>, limits[0]);
-            if (runs_of(s.T, V) == 1) return launch(resident_gradient_kernel<IO, ACT, 1, kFewThreads, kGradientCtas>, limits[1]);
-            if (runs_of(s.T, V) < P) return launch(resident_gradient_kernel<IO, ACT, 2, kFewThreads, kGradientCtas>, limits[2]);
+            if (r.form == 1) return launch(resident_gradient_kernel<IO, ACT, 1, kFewThreads, kGradientCtas>, limits[1]);
+            if (r.form < P) return launch(resident_gradient_kernel<IO, ACT, 2, kFewThreads, kGradientCtas>, limits[2]);
             return launch(resident_gradient_kernel<IO, ACT, P, kFewThreads, kGradientCtas>, limits[3]);
         });
     });
