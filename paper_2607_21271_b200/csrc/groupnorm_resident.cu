@@ -5,6 +5,8 @@
 // group, written into every CTA's shared memory.  A thread stays with one 16-byte column, which it copies asynchronously into slots of its own: no
 // barrier stands between copy and use, as many bytes are in flight as shared memory holds, and a slot that has been read for the last
 // time takes a vector of the next instance at once.  What belongs to a column stays in registers for all instances that a CTA takes.
+#include <algorithm>
+
 #include "groupnorm_common.cuh"
 
 namespace eql {
@@ -556,7 +558,7 @@ ResidentNorm resident_norm_plan(const NormShape& s, eql_dtype_t dtype, bool back
     r.threads = columns <= kFewThreads ? kFewThreads : backward ? kManyBackward : kManyForward;
     r.form = r.threads == kFewThreads ? runs_of(s.T, V) : V / 2;              // (with many threads there is the general form only)
     r.blocks = (s.groups + r.groups - 1) / r.groups;
-    r.run = run_length(s.T, V);
+    r.run = std::min(run_length(s.T, V), V / r.form);         // (a thread of form N keeps N pairs of sums at least)
     r.sums = V / r.run;
     r.tuple = Divisor(s.T);
     r.width = Divisor(s.width);

@@ -73,6 +73,10 @@ def test_what_threads_put_side_by_side_has_room(dtype, V, backward):
             side = r.threads * (r.sums + entries) + channels if backward else max(r.threads * entries, 2 * r.threads // 32)
             assert r.side_offset >= r.slot_bytes + 8 * r.groups + 24 * r.cluster * r.groups, where
             assert r.side_offset + 8 * side <= r.shared_bytes <= SLOTS, where
+            if backward:
+                # a thread stores one sum of dz and dz * xh where N is 1, else one a run of N or two (each half of a pair)
+                assert r.sums in ((1,) if N == 1 else (N, 2 * N)) and r.sums * r.run == V, where
+                assert T % r.run == 0 and r.runs.d * r.run == T, where      # a sum is of one channel, whose sums follow each other
             lanes = r.lanes.d
             assert -(-r.rows // lanes) * r.threads * 16 * (2 if backward else 1) <= r.slot_bytes and r.rows * r.cluster >= S, where
             wide += r.threads > 256
