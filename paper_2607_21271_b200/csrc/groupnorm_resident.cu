@@ -121,8 +121,8 @@ __device__ __forceinline__ float warp_sum(float v) {
 __device__ __forceinline__ float element(const float2* v, int j) { return j % 2 ? v[j / 2].y : v[j / 2].x; }
 
 // Mean and squared distances of a warp's entries, each of n values, `count` in all.  at(e) gives an entry's n and its (mean, squared
-// distances).  The entries' means are taken relative to the average of the lanes' first ones, which a single far value moves by no
-// more than a 32nd of what it moves its own entry's mean (or by its share, of fewer entries).
+// distances); no entry is of no values.  The entries' means are taken relative to the average of the lanes' first ones, which a single far
+// value moves by no more than a 32nd of what it moves its own entry's mean (or by its share, of fewer entries).
 template <typename At>
 __device__ __forceinline__ Moments moments_of(float count, int entries, At&& at) {
     const int lane = threadIdx.x & 31;
@@ -256,7 +256,9 @@ __global__ void __launch_bounds__(THREADS, CTAS) resident_norm_kernel(NormShape 
             Moments t;
             const float count = (float)rows.all * s.width;
             if (whole && p.groups == 1) {
-                t = moments_of(count, warps, [&](int e, float* n) { *n = m.side[2 * e + 1].x; return m.side[2 * e]; });
+                // the warps that have rows: the threads that do are the first ones, lane by lane.  (An idle warp's mean of 0 in the entries'
+                // average costs far means their digits: 640 floats about 1000 with a spread of 1, three warps of eight idle, gave y up to 0.03 off.)
+                t = moments_of(count, (min(p.lanes, rows.all) * p.columns + 31) >> 5, [&](int e, float* n) { *n = m.side[2 * e + 1].x; return m.side[2 * e]; });
             } else {
                 // entries of a lane of rows: the group's vectors, or where they cross its border its runs
                 const int per = whole ? 1 : Runs<N, P>::kEntries, row = p.columns * per;

@@ -60,3 +60,16 @@ def test_wide_rows_in_padded_batches_give_the_same_bits_again(shape, dtype):
         again = n.outputs()
         assert all(torch.equal(first[k], again[k]) for k in first)
     n.guard.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lengths", [False, True])
+@pytest.mark.parametrize("shape", [(8, 80, 1, 5, 1), (8, 192, 1, 3, 1), (8, 256, 1, 3, 1), (8, 96, 1, 9, 40), (4, 8, 1, 9, 300), (1, 640, 1, 9, 8), (8, 160, 1, 6, 3),
+                                   (4, 514, 2, 5, 2)], ids=ids)
+def test_values_far_from_zero_where_warps_have_no_rows(shape, lengths):
+    """One group a block whose columns leave warps idle, and instances shorter than a CTA has rows: the spread is a thousandth of the mean."""
+    T, C, groups, B, S = shape
+    rng = np.random.default_rng(5)
+    n = Norm(*shape, "fp32", "none", seed=6, x=1000.0 + rng.standard_normal((B, S, C, T)),
+             lengths=[(1, 2, 3, S, 0)[i % 5] for i in range(B)] if lengths else None)
+    n.step()
