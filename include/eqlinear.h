@@ -417,11 +417,13 @@ eql_status_t eqlinear_adamw(eqlinear_adamw_t* opt, const eql_adamw_tensor_t* ten
  *   max_norm    > 0; infinity bounds nothing
  *   loss_scale  device float, read when the kernel runs, or NULL for 1
  *   norm        device float that receives n, or NULL
+ * Pageable memory of the host, or memory of another device, is refused for either (EQL_ERR_INVALID_ARG).
  * Squares and sums are doubles, added in a fixed order: the same gradients give the same bits. */
 eql_status_t eqlinear_adamw_clip(eqlinear_adamw_t opt, float max_norm, const float* loss_scale, float* norm, void* stream);
 
 /* One step over all tensors (one kernel); uses up what eqlinear_adamw_clip left.
- *   lr         >= 0, used unless lr_device is given: a device float, read when the kernel runs (schedules in captured graphs)
+ *   lr         >= 0, used unless lr_device is given: a device float, read when the kernel runs (schedules in captured
+ *              graphs); pageable memory of the host, or memory of another device, is refused (EQL_ERR_INVALID_ARG)
  *   beta1, beta2 in [0, 1);  eps at least 2^-126
  * The step number lives on the device and advances by itself, so a captured step can be replayed. */
 eql_status_t eqlinear_adamw_step(eqlinear_adamw_t opt, double lr, double beta1, double beta2, double eps,

@@ -562,6 +562,13 @@ bool on_device(const eql_adamw_tensor_t& t, int device) {
         if (!on_device(p, device)) return false;
     return true;
 }
+// Whether a kernel on `device` can reach a scalar (or there is none): pinned memory of the host counts, pageable memory does not.
+bool reachable(const void* p, int device) {
+    if (!p) return true;
+    cudaPointerAttributes a{};
+    if (cudaPointerGetAttributes(&a, p) != cudaSuccess) { cudaGetLastError(); return false; }
+    return a.type == cudaMemoryTypeManaged || a.type == cudaMemoryTypeHost || (a.type == cudaMemoryTypeDevice && a.device == device);
+}
 // Calls that wait for a stream cannot be captured.
 eql_status_t not_capturing(cudaStream_t s) {
     cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
@@ -687,6 +694,7 @@ eql_status_t eqlinear_adamw_clip(eqlinear_adamw_t opt, float max_norm, const flo
     if (eql_status_t st = check_optimiser(opt); st != EQL_OK) return st;
     if (!(max_norm > 0.0f)) return EQL_ERR_INVALID_ARG;
     if (!aligned(loss_scale, 4) || !aligned(norm, 4)) return EQL_ERR_ALIGNMENT;
+    if (!reachable(loss_scale, opt->device) || !reachable(norm, opt->device)) return EQL_ERR_INVALID_ARG;
     const int64_t most = std::min(opt->num_sms * kNormCtasPerSm, kMaxNormCtas);
     const unsigned grid = (unsigned)std::max<int64_t>(1, std::min(opt->lay.n_chunks, most));
     const auto kernel = opt->grad_dtype == kMixed ? grad_norm_kernel<kMixed> : opt->grad_dtype == EQL_FP32 ? grad_norm_kernel<EQL_FP32>
@@ -701,6 +709,7 @@ eql_status_t eqlinear_adamw_step(eqlinear_adamw_t opt, double lr, double beta1, 
     if (!(lr >= 0.0) || !std::isfinite((float)lr) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0)) return EQL_ERR_INVALID_ARG;
     if (!((float)eps >= FLT_MIN) || !std::isfinite((float)eps)) return EQL_ERR_INVALID_ARG;
     if (!aligned(lr_device, 4)) return EQL_ERR_ALIGNMENT;
+    if (!reachable(lr_device, opt->device)) return EQL_ERR_INVALID_ARG;
     const Rates r{(float)lr, (float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps, 1.0f, std::log(beta1), std::log(beta2), lr_device};
     const int64_t most = (int64_t)opt->num_sms * step_ctas_per_sm(opt->state_bits);
     const unsigned grid = (unsigned)std::max<int64_t>(1, std::min(opt->lay.n_chunks, most));

@@ -514,3 +514,31 @@ def test_a_loss_scale_whose_reciprocal_is_not_finite_changes_nothing():
         assert all(torch.equal(a[k], b[k]) for a, b in zip(before, o.snapshot()) for k in a)
     finally:
         o.close()
+
+
+@pytest.mark.gpu
+def test_scalars_that_a_kernel_cannot_reach_are_refused():
+    """A learning rate, loss scale or norm in ordinary memory of the host is refused before any launch; pinned memory is read and written."""
+    o = Optimiser((300, 7), "fp32", "fp32", 32, False, seed=14)
+    try:
+        host, before = torch.full((1,), 1e-3), o.snapshot()
+        for call in (lambda: eq.eqlinear_adamw_step(o.h, 1e-3, lr_device=host, stream=o.stream),
+                     lambda: eq.eqlinear_adamw_clip(o.h, 1.0, loss_scale=host, stream=o.stream),
+                     lambda: eq.eqlinear_adamw_clip(o.h, 1.0, norm=host, stream=o.stream)):
+            with pytest.raises(eq.EqlError) as e:
+                call()
+            assert e.value.status == binding.EQL_ERR_INVALID_ARG
+        info = eq.eqlinear_adamw_info(o.h, o.stream)
+        assert (info.step, info.skipped, info.skip) == (0, 0, 0) and float(host) == float(torch.tensor(1e-3))
+        assert all(torch.equal(a[k], b[k]) for a, b in zip(before, o.snapshot()) for k in a)
+        norm, lr = torch.zeros(1).pin_memory(), torch.full((1,), 1e-3).pin_memory()
+        want = reference(o, 1, float(lr), 0.9, 0.999, 1e-8)
+        eq.eqlinear_adamw_clip(o.h, math.inf, norm=norm, stream=o.stream)
+        eq.eqlinear_adamw_step(o.h, 7.0, lr_device=lr, stream=o.stream)
+        o.check_guards()
+        total = math.sqrt(sum(float(t["g"].double().square().sum()) for t in o.parts))
+        assert abs(float(norm) - total) <= U * total * 1.001
+        for part, ((p, ep), _, _) in zip(o.parts, want):
+            within(part["p"], p, ep)
+    finally:
+        o.close()
