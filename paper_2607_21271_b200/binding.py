@@ -358,6 +358,8 @@ def eqlinear_adamw_clip(opt, max_norm, loss_scale=None, norm=None, stream=0) -> 
 
 
 def eqlinear_adamw_step(opt, lr, beta1=0.9, beta2=0.999, eps=1e-8, lr_device=None, stream=0) -> None:
+    """One step.  The default beta2 is for states in 32 bits: second moments in 8 bits follow their gradients up to beta2 = 0.95 (codes are
+    rounded to nearest, and a smaller change than half a step between codes leaves them where they are)."""
     _check(load_library().eqlinear_adamw_step(opt, lr, beta1, beta2, eps, _ptr(lr_device), stream or None), "eqlinear_adamw_step")
 
 

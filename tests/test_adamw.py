@@ -542,3 +542,43 @@ def test_scalars_that_a_kernel_cannot_reach_are_refused():
             within(part["p"], p, ep)
     finally:
         o.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("beta2", [0.8, 0.9, 0.95])
+def test_eight_bit_second_moments_follow_changing_gradients(beta2):
+    """Hundreds of steps, then gradients of a quarter of each block three times smaller and of another quarter three times larger: sqrt(v) stays
+    near that of 64 bits.
+
+    Codes lie 14 to 25 % apart, so a step's rounding moves v by an error of standard deviation 0.25 / sqrt(12) of v at most, which
+    decays by beta2 a step: 0.25 / sqrt(12 (1 - beta2^2)) altogether if the roundings are independent, half of that for the root."""
+    blocks, steps = 24, 600
+    n = blocks * BLOCK
+    gen = torch.Generator(device="cuda").manual_seed(15)
+    rand = lambda: torch.randn(n, device="cuda", generator=gen)                       # noqa: E731
+    p, g = rand(), torch.zeros(n, device="cuda")
+    m, v = (torch.zeros(n, dtype=torch.uint8, device="cuda") for _ in range(2))
+    ms, vs = (torch.zeros(blocks, device="cuda") for _ in range(2))
+    table = [eq.eqlinear_adamw_tensor(p, g, m, v, n, eq.EQL_FP32, eq.EQL_FP32, exp_avg_scale=ms, exp_avg_sq_scale=vs)]
+    bytes_ = eq.eqlinear_adamw_workspace_bytes(table, 8)
+    workspace = torch.empty(bytes_, dtype=torch.uint8, device="cuda")
+    s = torch.cuda.current_stream().cuda_stream
+    h = eq.eqlinear_adamw(table, 8, workspace, bytes_, s)
+    try:
+        size, part = torch.exp(rand()), torch.arange(n, device="cuda") % 4
+        want = torch.zeros(n, dtype=torch.float64, device="cuda")
+        sigma = 0.5 * 0.25 / math.sqrt(12 * (1 - beta2 ** 2))
+        for factors in ((1.0, 1.0), (1 / 3, 3.0)):
+            now = torch.where(part == 0, size * factors[0], torch.where(part == 1, size * factors[1], size))
+            for _ in range(steps):
+                g.copy_(now * rand())
+                want.mul_(beta2).add_(g.double().square(), alpha=1 - beta2)
+                eq.eqlinear_adamw_step(h, 1e-3, 0.9, beta2, stream=s)
+            held = v.view(torch.float8_e5m2).double() * vs.double().repeat_interleave(BLOCK)
+            off = torch.log(held / want) / 2                                          # of the root, relative
+            for k in range(4):
+                assert float(off[part == k].mean().abs()) < sigma / 3                 # a mean over 1536 of them: nothing drags behind
+            assert float(off.std()) < 1.5 * sigma and float(off.abs().max()) < 6 * sigma
+    finally:
+        torch.cuda.synchronize()
+        eq.eqlinear_adamw_destroy(h)
