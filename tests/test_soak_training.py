@@ -91,3 +91,70 @@ def test_random_norms(seed):
     B = max(1, rows // S)
     lengths = rng.integers(0, S + 1, B) if rng.random() < 0.4 else None
     Norm(T, C, groups, B, S, dtype, ("none", "gelu", "silu")[int(rng.integers(3))], lengths=lengths, seed=seed).step()
+
+
+@pytest.mark.parametrize("T,C,groups,B,S", [(8, 96, 1, 3_200_000, 1), (8, 96, 32, 16_300, 197), (16, 64, 1, 1, 2_200_000)])
+def test_parameter_gradients_over_tensors_beyond_four_gigabytes(T, C, groups, B, S):
+    """All of dgamma and dbeta, and dx at a few instances or rows, against the formulas in 64 bits from x, dy and the statistics given."""
+    D = C * T
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    x, dy, dx = (torch.empty(B * S, D, dtype=torch.float16, device="cuda") for _ in range(3))
+    assert x.numel() * 2 > 1 << 32
+    step = (1 << 16) // S * S or 1 << 16                      # whole instances, or rows of the one map
+    for r in range(0, B * S, step):
+        x[r:r + step].normal_(generator=gen)
+        dy[r:r + step].normal_(generator=gen)
+    gamma, beta = (torch.randn(C, device="cuda", generator=gen).half() for _ in range(2))
+    stats = torch.stack([0.1 * torch.randn(B, groups, device="cuda", generator=gen), 1 + 0.1 * torch.rand(B, groups, device="cuda", generator=gen)], -1)
+    dgamma, dbeta = torch.empty(C, device="cuda"), torch.empty(C, device="cuda")
+    desc = eq.eqlinear_groupnorm_desc(T, C, groups, eq.EQL_FP16, B, S, act=ACTS["silu"], eps=EPS)
+    bytes_ = eq.eqlinear_groupnorm_scratch_bytes(desc)
+    scratch = torch.empty(max(256, bytes_), dtype=torch.uint8, device="cuda")
+    eq.eqlinear_groupnorm_bwd(desc, x, dy, gamma, beta, None, stats, dx, dgamma, dbeta, scratch, bytes_)
+    torch.cuda.synchronize()
+    want = torch.zeros(2, C, dtype=torch.float64, device="cuda")
+    squares = torch.zeros(2, C, dtype=torch.float64, device="cuda")
+    ga, be = (p.double().view(1, groups, C // groups, 1) for p in (gamma, beta))
+
+    def parts(r, end):
+        """xh and dz of rows r to end, [rows, groups, channels, tuple]"""
+        st = stats[r // S:-(-end // S)].double().repeat_interleave(min(S, end - r), 0).view(end - r, groups, 1, 1, 2)
+        xh = (x[r:end].double().view(end - r, groups, C // groups, T) - st[..., 0]) * st[..., 1]
+        z = xh * ga + be
+        p = torch.sigmoid(z)
+        return xh, dy[r:end].double().view_as(xh) * p * (1 + z * (1 - p)), st[..., 1]
+
+    for r in range(0, B * S, step):
+        xh, dz, _ = parts(r, min(B * S, r + step))
+        for k, term in enumerate((dz * xh, dz)):
+            want[k] += term.sum((0, 3)).view(C)
+            squares[k] += term.square().sum((0, 3)).view(C)
+    # n roundings, independent, of partial sums no larger than 6 standard deviations of the whole one: 6 rms sqrt(n) * U * sqrt(n)
+    n = B * S * T
+    for got, w, sq in zip((dgamma, dbeta), want, squares):
+        assert bool(((got.double() - w).abs() <= 8 * 2.0 ** -24 * n * torch.sqrt(sq / n)).all())
+        assert float(w.abs().max()) > 100 * 8 * 2.0 ** -24 * n * float(torch.sqrt(sq / n).max())       # what an instance more or less would show in
+    if B == 1:
+        s1, s2 = (ga.view(C) * want[1]).sum() / (S * D), (ga.view(C) * want[0]).sum() / (S * D)
+        for row in ((1 << 31) // (2 * D), (1 << 32) // (2 * D), S - 1):
+            xh, dz, rstd = parts(row, row + 1)
+            value = (rstd * (ga * dz - s1 - xh * s2)).view(D)
+            assert bool(((dx[row].double() - value).abs() <= 2.0 ** -11 * value.abs() + 1e-5).all())    # half's rounding, and float's of values below 100
+
+
+@pytest.mark.parametrize("seed", range(90))
+def test_random_norms_of_wide_rows(seed):
+    """Rows of a thousand to ten thousand elements: all kernels' borders, with tuples and groups of every kind."""
+    rng = np.random.default_rng(5000 + seed)
+    dtype = ("fp32", "fp16", "bf16")[seed % 3]
+    size = 4 if dtype == "fp32" else 2
+    T = int(rng.choice([1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 16, 20, 32]))
+    step = next(k for k in range(1, 17) if k * T * size % 16 == 0)
+    C = int(step * max(1, round(np.exp(rng.uniform(np.log(1000), np.log(10000))) / (T * step))))
+    few = [g for g in range(1, 9) if C % g == 0]
+    groups = int(rng.choice(few if rng.random() < 0.8 else [g for g in range(1, min(C, 64) + 1) if C % g == 0]))
+    rows = int(np.exp(rng.uniform(0, np.log(600_000 / (C * T) + 2)))) + 1
+    S = int(rng.choice([1, rng.integers(1, rows + 1), rows]))
+    B = max(1, rows // S)
+    lengths = rng.integers(0, S + 1, B) if rng.random() < 0.4 else None
+    Norm(T, C, groups, B, S, dtype, ("none", "gelu", "silu")[int(rng.integers(3))], lengths=lengths, seed=seed).step()
