@@ -246,6 +246,7 @@ __device__ __forceinline__ void update(const Formula& f, Fetched<BITS>& b, int g
     most_m = warp_max(most_m);
     most_v = warp_max(most_v);
     const bool fine_m = !(most_m < kTiny), fine_v = !(most_v < kTiny);
+    // (To nearest: what a step moves by less than half of what lies between codes keeps its code.  That bounds beta2, see eqlinear.h.)
     // the block's four divisions, each in another lane: the inverse scales of m and v, and the scales
     const int lane = threadIdx.x & 31;
     const bool of_v = lane & 1, scale = lane & 2;
